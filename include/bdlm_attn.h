@@ -218,6 +218,49 @@ int bdlm_attn_bwd_packed(const bdlm_params* p, const bdlm_packed_geometry* g,
                          void* dq_noisy, void* dk_noisy, void* dv_noisy,
                          void* workspace, size_t workspace_bytes, void* cuda_stream);
 
+/*
+ * Packed documents: the packed form over a sequence made of several documents, none of which sees another.
+ *
+ *   - The documents lie one after the other along the clean positions: document i holds the positions
+ *     cu_seqlens[i] .. cu_seqlens[i + 1] - 1.  Every rule above applies inside a document: a clean query sees the clean
+ *     keys of its own document only (of any length, one token included), and a corrupted block belongs to the document
+ *     of the position it starts at, block_prefix[b], and sees that document's clean keys before it (none, where
+ *     block_prefix[b] is the document's first position).  Position L belongs to no document.
+ *   - bdlm_doc_table writes the table that the kernels read, once for a packed batch; the layers' calls, forward and
+ *     backward, share it.  It is the same for all batch elements.  cu_seqlens is a DEVICE array of n_docs + 1
+ *     non-decreasing int32 in [0, L] (empty documents are allowed); its values are not validated, wrong ones give wrong
+ *     masks but no access outside the tensors.  Positions before the first and from the last entry on belong to no document:
+ *     clean rows there see nothing (O = 0, LSE = -inf, zero gradients), but like all rows they have to hold finite values,
+ *     because the products run over whole tiles.
+ *   - With q_noisy NULL this is causal attention over prompts of different lengths (block_size is then unused: pass 1).
+ *   - kv_chunk_len > 0 is not offered together with documents (BDLM_ERR_UNSUPPORTED).  Workspace, statuses, layouts and
+ *     reproducibility are those of bdlm_attn_fwd_packed / bdlm_attn_bwd_packed (bdlm_workspace_bytes_packed).
+ */
+typedef struct {
+  const int32_t* table;   /* device, [L + 1][2] int32, 8-byte aligned, as bdlm_doc_table wrote it */
+  int32_t max_len;        /* tokens of the longest document; chooses launch shapes, never results' meaning.  0 = not known */
+  int32_t reserved;       /* 0 */
+  int64_t pairs;          /* sum of n (n + 1) / 2 over the documents' lengths n; likewise.  0 = not known */
+} bdlm_docs;
+
+int bdlm_doc_table(const int32_t* cu_seqlens, int32_t n_docs, int32_t L, int32_t* table, void* cuda_stream);
+
+int bdlm_attn_fwd_docs(const bdlm_params* p, const bdlm_packed_geometry* g, const bdlm_docs* docs,
+                       const void* q_clean, const void* k_clean, const void* v_clean,
+                       const void* q_noisy, const void* k_noisy, const void* v_noisy,
+                       void* o_clean, void* o_noisy, float* lse_clean, float* lse_noisy,
+                       void* cuda_stream);
+
+int bdlm_attn_bwd_docs(const bdlm_params* p, const bdlm_packed_geometry* g, const bdlm_docs* docs,
+                       const void* q_clean, const void* k_clean, const void* v_clean,
+                       const void* q_noisy, const void* k_noisy, const void* v_noisy,
+                       const void* o_clean, const void* o_noisy,
+                       const float* lse_clean, const float* lse_noisy,
+                       const void* do_clean, const void* do_noisy,
+                       void* dq_clean, void* dk_clean, void* dv_clean,
+                       void* dq_noisy, void* dk_noisy, void* dv_noisy,
+                       void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 /* Human-readable name of a status code (static storage). */
 const char* bdlm_status_string(int status);
 

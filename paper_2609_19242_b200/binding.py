@@ -24,7 +24,7 @@ EXPORTS = ("bdlm_workspace_bytes", "bdlm_attn_fwd", "bdlm_attn_bwd", "bdlm_lse_m
            "bdlm_status_string", "bdlm_get_device_status", "bdlm_set_trace_buffer",
            "bdlm_attn_bwd_static_scratch", "bdlm_workspace_bytes_packed", "bdlm_attn_fwd_packed",
            "bdlm_attn_bwd_packed", "bdlm_selftest_wait_timeout", "bdlm_linear_ce_workspace_bytes",
-           "bdlm_linear_ce_fwd", "bdlm_linear_ce_bwd")
+           "bdlm_linear_ce_fwd", "bdlm_linear_ce_bwd", "bdlm_doc_table", "bdlm_attn_fwd_docs", "bdlm_attn_bwd_docs")
 LCE_WS_FWD, LCE_WS_BWD, LCE_WS_FWD_LEAST, LCE_WS_BWD_LEAST = 0, 1, 2, 3
 STATIC_SCRATCH_ROWS = 1 << 20
 TRACE_SLOTS = 256
@@ -50,6 +50,10 @@ class BdlmPackedGeometry(ctypes.Structure):
     _fields_ = [("Lq_clean", ctypes.c_int32), ("clean_q_pos0", ctypes.c_int32), ("n_blocks", ctypes.c_int32),
                 ("kv_chunk_len", ctypes.c_int32), ("block_prefix", ctypes.c_void_p),
                 ("kv_chunk_pos", ctypes.c_void_p), ("kv_pos_chunk", ctypes.c_void_p)]
+
+
+class BdlmDocs(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("max_len", ctypes.c_int32), ("reserved", ctypes.c_int32), ("pairs", ctypes.c_int64)]
 
 
 class BdlmLceParams(ctypes.Structure):
@@ -93,6 +97,13 @@ def lib():
         L.bdlm_attn_fwd_packed.argtypes = [pp, gp] + [vp] * 10 + [vp]
         L.bdlm_attn_bwd_packed.restype = ctypes.c_int
         L.bdlm_attn_bwd_packed.argtypes = [pp, gp] + [vp] * 18 + [vp, ctypes.c_size_t, vp]
+        dp = ctypes.POINTER(BdlmDocs)
+        L.bdlm_doc_table.restype = ctypes.c_int
+        L.bdlm_doc_table.argtypes = [vp, ctypes.c_int32, ctypes.c_int32, vp, vp]
+        L.bdlm_attn_fwd_docs.restype = ctypes.c_int
+        L.bdlm_attn_fwd_docs.argtypes = [pp, gp, dp] + [vp] * 10 + [vp]
+        L.bdlm_attn_bwd_docs.restype = ctypes.c_int
+        L.bdlm_attn_bwd_docs.argtypes = [pp, gp, dp] + [vp] * 18 + [vp, ctypes.c_size_t, vp]
         lp = ctypes.POINTER(BdlmLceParams)
         L.bdlm_linear_ce_workspace_bytes.restype = ctypes.c_size_t
         L.bdlm_linear_ce_workspace_bytes.argtypes = [lp, ctypes.c_int32]
@@ -135,6 +146,14 @@ def _ptr(t):
 
 def _stream():
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
+
+def _on_current_device(t):
+    """Launches go to the current device's stream: memory of another one would be out of the kernels' reach."""
+    if not t.is_cuda:
+        raise ValueError("tensors must be CUDA tensors")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on {t.device}, which is not the current device")
 
 
 def _shape_params(q, k, block_size, **kw):
@@ -301,13 +320,61 @@ def _packed_setup(q_clean, k_clean, q_noisy, block_size, block_prefix, clean_q_p
     return p, g
 
 
+class DocTable:
+    """The table of a packed batch's documents (bdlm_doc_table): `table` int32 [L + 1, 2] on the device, `struct` what the
+    library is handed.  One table serves every layer's forward and backward of the batch."""
+
+    def __init__(self, table, L, max_len, pairs):
+        self.table, self.L, self.max_len, self.pairs = table, L, max_len, pairs
+        self.struct = BdlmDocs(table.data_ptr(), max_len, 0, pairs)
+
+
+def bdlm_doc_table(cu_seqlens, L=None, device=None) -> DocTable:
+    """Table of the documents of a packed sequence of L clean positions (default: the last entry).  `cu_seqlens`: n + 1
+    non-decreasing starts and ends in [0, L], int32, or a list; document i holds positions cu_seqlens[i] ..
+    cu_seqlens[i + 1] - 1, positions outside all of them see nothing.  Its values are checked here, on a host copy, so a CUDA
+    tensor makes the call wait for the device: hand over the host's."""
+    cu = torch.as_tensor(cu_seqlens)
+    if cu.dim() != 1 or cu.numel() < 2 or cu.dtype not in (torch.int32, torch.int64):
+        raise ValueError("cu_seqlens must be one-dimensional int32 (or int64) with at least two entries")
+    device = torch.device(device if device is not None else cu.device if cu.is_cuda else "cuda")
+    host = cu.cpu().long()
+    L = int(host[-1]) if L is None else int(L)
+    lens = host[1:] - host[:-1]
+    if int(host[0]) < 0 or int(host[-1]) > L or int(lens.min()) < 0:
+        raise ValueError("cu_seqlens must be non-decreasing and lie in [0, L]")
+    if L <= 0 or L > 1 << 30:
+        raise ValueError("L must lie in [1, 2**30]")
+    with torch.cuda.device(device):
+        dev = cu.to(device=device, dtype=torch.int32).contiguous()
+        table = torch.empty(L + 1, 2, dtype=torch.int32, device=device)
+        rc = lib().bdlm_doc_table(_ptr(dev), dev.numel() - 1, L, _ptr(table), _stream())
+    if rc != 0:
+        raise BdlmError(rc, "bdlm_doc_table")
+    return DocTable(table, L, int(lens.max()), int((lens * (lens + 1) // 2).sum()))
+
+
+def _check_docs(docs, k_clean, kv_chunks):
+    _on_current_device(k_clean)
+    if docs.L != k_clean.shape[1]:
+        raise ValueError("the table of documents is for another number of clean positions")
+    if docs.table.device != k_clean.device:
+        raise ValueError("the table of documents is on another device")
+    if kv_chunks is not None:
+        raise ValueError("documents and gathered clean K/V (kv_chunks) cannot be combined")
+
+
 def bdlm_attn_fwd_packed(q_clean, k_clean, v_clean, q_noisy, k_noisy, v_noisy, block_size, *,
                          block_prefix=None, clean_q_pos0=0, out=None, scale=0.0, clean_mask_mode=0,
-                         kv_range=None, include_noisy_diag=True, impl=IMPL_AUTO, window=0, kv_chunks=None):
+                         kv_range=None, include_noisy_diag=True, impl=IMPL_AUTO, window=0, kv_chunks=None, docs=None):
     """Forward of the packed form (one rank's launch of the CSBP schedule; DFlash2-style blocks).
     q_clean [batch, Lq, H, d] or None: clean queries at positions clean_q_pos0 .. ; q_noisy
     [batch, n_blocks*block_size, H, d] or None with k_noisy/v_noisy packed alike; k_clean/v_clean
-    [batch, L, H_kv, d] complete.  Returns (o_clean, lse_clean, o_noisy, lse_noisy)."""
+    [batch, L, H_kv, d] complete.  `docs` (a DocTable): the sequence is made of documents, none of which sees another;
+    with q_noisy None and block_size 1 that is causal attention over prompts of different lengths.
+    Returns (o_clean, lse_clean, o_noisy, lse_noisy)."""
+    if docs is not None:
+        _check_docs(docs, k_clean, kv_chunks)
     p, g = _packed_setup(q_clean, k_clean, q_noisy, block_size, block_prefix, clean_q_pos0, window, kv_chunks,
                          scale=scale, clean_mask_mode=clean_mask_mode, kv_range=kv_range,
                          include_noisy_diag=include_noisy_diag, impl=impl)
@@ -317,21 +384,26 @@ def bdlm_attn_fwd_packed(q_clean, k_clean, v_clean, q_noisy, k_noisy, v_noisy, b
         mk_l = lambda q: None if q is None else torch.empty(p.batch, p.H, q.shape[1], dtype=torch.float32, device=dev)
         out = (mk_o(q_clean), mk_l(q_clean), mk_o(q_noisy), mk_l(q_noisy))
     o_c, l_c, o_n, l_n = out
-    rc = lib().bdlm_attn_fwd_packed(ctypes.byref(p), ctypes.byref(g), _ptr(q_clean), _ptr(k_clean), _ptr(v_clean),
-                                    _ptr(q_noisy), _ptr(k_noisy), _ptr(v_noisy),
-                                    _ptr(o_c), _ptr(o_n), _ptr(l_c), _ptr(l_n), _stream())
+    args = (_ptr(q_clean), _ptr(k_clean), _ptr(v_clean), _ptr(q_noisy), _ptr(k_noisy), _ptr(v_noisy),
+            _ptr(o_c), _ptr(o_n), _ptr(l_c), _ptr(l_n), _stream())
+    if docs is None:
+        rc = lib().bdlm_attn_fwd_packed(ctypes.byref(p), ctypes.byref(g), *args)
+    else:
+        rc = lib().bdlm_attn_fwd_docs(ctypes.byref(p), ctypes.byref(g), ctypes.byref(docs.struct), *args)
     if rc != 0:
-        raise BdlmError(rc, "bdlm_attn_fwd_packed")
+        raise BdlmError(rc, "bdlm_attn_fwd_packed" if docs is None else "bdlm_attn_fwd_docs")
     return o_c, l_c, o_n, l_n
 
 
 def bdlm_attn_bwd_packed(q_clean, k_clean, v_clean, q_noisy, k_noisy, v_noisy, o_clean, lse_clean,
                          o_noisy, lse_noisy, do_clean, do_noisy, block_size, *, block_prefix=None,
                          clean_q_pos0=0, out=None, workspace=None, scale=0.0, clean_mask_mode=0,
-                         impl=IMPL_AUTO, passes=0, single_pass=None, window=0, kv_chunks=None):
-    """Backward of the packed form.  Returns (dq_clean, dk_clean, dv_clean, dq_noisy, dk_noisy, dv_noisy);
+                         impl=IMPL_AUTO, passes=0, single_pass=None, window=0, kv_chunks=None, docs=None):
+    """Backward of the packed form (`docs` as in the forward).  Returns (dq_clean, dk_clean, dv_clean, dq_noisy, dk_noisy, dv_noisy);
     entries of a stream that was left out are None.  dk_clean/dv_clean are this call's contribution for
     every clean key.  `single_pass` as in bdlm_attn_bwd."""
+    if docs is not None:
+        _check_docs(docs, k_clean, kv_chunks)
     p, g = _packed_setup(q_clean, k_clean, q_noisy, block_size, block_prefix, clean_q_pos0, window, kv_chunks,
                          scale=scale, clean_mask_mode=clean_mask_mode, impl=impl, bwd_passes=passes,
                          bwd_single_pass=single_pass)
@@ -343,13 +415,15 @@ def bdlm_attn_bwd_packed(q_clean, k_clean, v_clean, q_noisy, k_noisy, v_noisy, o
     if workspace is None:
         workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=k_clean.device)
     dq_c, dk_c, dv_c, dq_n, dk_n, dv_n = out
-    rc = lib().bdlm_attn_bwd_packed(ctypes.byref(p), ctypes.byref(g), _ptr(q_clean), _ptr(k_clean), _ptr(v_clean),
-                                    _ptr(q_noisy), _ptr(k_noisy), _ptr(v_noisy), _ptr(o_clean), _ptr(o_noisy),
-                                    _ptr(lse_clean), _ptr(lse_noisy), _ptr(do_clean), _ptr(do_noisy),
-                                    _ptr(dq_c), _ptr(dk_c), _ptr(dv_c), _ptr(dq_n), _ptr(dk_n), _ptr(dv_n),
-                                    _ptr(workspace), workspace.numel(), _stream())
+    args = (_ptr(q_clean), _ptr(k_clean), _ptr(v_clean), _ptr(q_noisy), _ptr(k_noisy), _ptr(v_noisy), _ptr(o_clean), _ptr(o_noisy),
+            _ptr(lse_clean), _ptr(lse_noisy), _ptr(do_clean), _ptr(do_noisy),
+            _ptr(dq_c), _ptr(dk_c), _ptr(dv_c), _ptr(dq_n), _ptr(dk_n), _ptr(dv_n), _ptr(workspace), workspace.numel(), _stream())
+    if docs is None:
+        rc = lib().bdlm_attn_bwd_packed(ctypes.byref(p), ctypes.byref(g), *args)
+    else:
+        rc = lib().bdlm_attn_bwd_docs(ctypes.byref(p), ctypes.byref(g), ctypes.byref(docs.struct), *args)
     if rc != 0:
-        raise BdlmError(rc, "bdlm_attn_bwd_packed")
+        raise BdlmError(rc, "bdlm_attn_bwd_packed" if docs is None else "bdlm_attn_bwd_docs")
     return out
 
 

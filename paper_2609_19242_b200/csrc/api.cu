@@ -58,7 +58,14 @@ int check_params(const bdlm_params* p, const bdlm_packed_geometry* g = nullptr) 
   return BDLM_OK;
 }
 
-void fill(KArgs& a, const bdlm_params* p, const bdlm_packed_geometry* g) {
+int check_docs(const bdlm_packed_geometry* g, const bdlm_docs* docs) {
+  if (docs == nullptr || docs->table == nullptr || (reinterpret_cast<uintptr_t>(docs->table) & 7u)) return BDLM_ERR_INVALID_ARG;
+  if (docs->max_len < 0 || docs->pairs < 0 || docs->reserved != 0) return BDLM_ERR_INVALID_ARG;
+  if (g->kv_chunk_len > 0) return BDLM_ERR_UNSUPPORTED;   // a document's first key tile may start anywhere: it would straddle chunks
+  return BDLM_OK;
+}
+
+void fill(KArgs& a, const bdlm_params* p, const bdlm_packed_geometry* g, const bdlm_docs* docs) {
   a.batch = p->batch; a.L = p->L; a.M = p->block_size; a.H = p->H; a.Hkv = p->H_kv;
   a.G = p->H / p->H_kv; a.d = p->d;
   if (g == nullptr) {
@@ -69,6 +76,9 @@ void fill(KArgs& a, const bdlm_params* p, const bdlm_packed_geometry* g) {
     a.Lqc = g->Lq_clean; a.cq_pos0 = g->clean_q_pos0; a.nb = g->n_blocks; a.Ln = g->n_blocks * p->block_size;
     a.prefix = g->block_prefix;
   }
+  a.docs = docs != nullptr ? reinterpret_cast<const int2*>(docs->table) : nullptr;
+  a.doc_max = docs != nullptr ? (docs->max_len > 0 && docs->max_len < p->L ? docs->max_len : p->L) : 0;
+  a.doc_pairs = docs != nullptr ? (double)docs->pairs : 0;
   a.scale = p->scale > 0.f ? p->scale : 1.0f / sqrtf((float)p->d);
   a.scale_log2 = a.scale * LOG2E;
   a.mode = p->clean_mask_mode;
@@ -134,7 +144,7 @@ size_t bdlm_workspace_bytes(const bdlm_params* p, int32_t which) {
   return 0;
 }
 
-static int fwd_impl(const bdlm_params* p, const bdlm_packed_geometry* g,
+static int fwd_impl(const bdlm_params* p, const bdlm_packed_geometry* g, const bdlm_docs* docs,
                     const void* q_clean, const void* k_clean, const void* v_clean,
                     const void* q_noisy, const void* k_noisy, const void* v_noisy,
                     void* o_clean, void* o_noisy, float* lse_clean, float* lse_noisy, void* cuda_stream) {
@@ -151,7 +161,7 @@ static int fwd_impl(const bdlm_params* p, const bdlm_packed_geometry* g,
   if (!is_sm100()) return BDLM_ERR_UNSUPPORTED;
 
   KArgs a;
-  fill(a, p, g);
+  fill(a, p, g, docs);
   using bf = __nv_bfloat16;
   a.q[CLEAN] = (const bf*)q_clean; a.q[NOISY] = (const bf*)q_noisy;
   a.k[CLEAN] = (const bf*)k_clean; a.k[NOISY] = (const bf*)(k_noisy ? k_noisy : k_clean);
@@ -168,7 +178,7 @@ static int fwd_impl(const bdlm_params* p, const bdlm_packed_geometry* g,
   return e == cudaSuccess ? BDLM_OK : BDLM_ERR_CUDA;
 }
 
-static int bwd_impl(const bdlm_params* p, const bdlm_packed_geometry* g,
+static int bwd_impl(const bdlm_params* p, const bdlm_packed_geometry* g, const bdlm_docs* docs,
                     const void* q_clean, const void* k_clean, const void* v_clean,
                     const void* q_noisy, const void* k_noisy, const void* v_noisy,
                     const void* o_clean, const void* o_noisy,
@@ -203,7 +213,7 @@ static int bwd_impl(const bdlm_params* p, const bdlm_packed_geometry* g,
   if (!is_sm100()) return BDLM_ERR_UNSUPPORTED;
 
   KArgs a;
-  fill(a, p, g);
+  fill(a, p, g, docs);
   using bf = __nv_bfloat16;
   a.q[CLEAN] = has_c ? (const bf*)q_clean : nullptr; a.q[NOISY] = has_n ? (const bf*)q_noisy : nullptr;
   a.k[CLEAN] = (const bf*)k_clean; a.k[NOISY] = has_n ? (const bf*)k_noisy : nullptr;
@@ -244,7 +254,7 @@ int bdlm_attn_fwd(const bdlm_params* p,
                   void* o_clean, void* o_noisy, float* lse_clean, float* lse_noisy,
                   void* workspace, size_t workspace_bytes, void* cuda_stream) {
   (void)workspace; (void)workspace_bytes;
-  return fwd_impl(p, nullptr, q_clean, k_clean, v_clean, q_noisy, k_noisy, v_noisy, o_clean, o_noisy,
+  return fwd_impl(p, nullptr, nullptr, q_clean, k_clean, v_clean, q_noisy, k_noisy, v_noisy, o_clean, o_noisy,
                   lse_clean, lse_noisy, cuda_stream);
 }
 
@@ -254,7 +264,7 @@ int bdlm_attn_fwd_packed(const bdlm_params* p, const bdlm_packed_geometry* g,
                          void* o_clean, void* o_noisy, float* lse_clean, float* lse_noisy,
                          void* cuda_stream) {
   if (g == nullptr) return BDLM_ERR_INVALID_ARG;
-  return fwd_impl(p, g, q_clean, k_clean, v_clean, q_noisy, k_noisy, v_noisy, o_clean, o_noisy,
+  return fwd_impl(p, g, nullptr, q_clean, k_clean, v_clean, q_noisy, k_noisy, v_noisy, o_clean, o_noisy,
                   lse_clean, lse_noisy, cuda_stream);
 }
 
@@ -267,7 +277,7 @@ int bdlm_attn_bwd(const bdlm_params* p,
                   void* dq_clean, void* dk_clean, void* dv_clean,
                   void* dq_noisy, void* dk_noisy, void* dv_noisy,
                   void* workspace, size_t workspace_bytes, void* cuda_stream) {
-  return bwd_impl(p, nullptr, q_clean, k_clean, v_clean, q_noisy, k_noisy, v_noisy, o_clean, o_noisy, lse_clean,
+  return bwd_impl(p, nullptr, nullptr, q_clean, k_clean, v_clean, q_noisy, k_noisy, v_noisy, o_clean, o_noisy, lse_clean,
                   lse_noisy, do_clean, do_noisy, dq_clean, dk_clean, dv_clean, dq_noisy, dk_noisy, dv_noisy,
                   workspace, workspace_bytes, cuda_stream);
 }
@@ -282,7 +292,43 @@ int bdlm_attn_bwd_packed(const bdlm_params* p, const bdlm_packed_geometry* g,
                          void* dq_noisy, void* dk_noisy, void* dv_noisy,
                          void* workspace, size_t workspace_bytes, void* cuda_stream) {
   if (g == nullptr) return BDLM_ERR_INVALID_ARG;
-  return bwd_impl(p, g, q_clean, k_clean, v_clean, q_noisy, k_noisy, v_noisy, o_clean, o_noisy, lse_clean,
+  return bwd_impl(p, g, nullptr, q_clean, k_clean, v_clean, q_noisy, k_noisy, v_noisy, o_clean, o_noisy, lse_clean,
+                  lse_noisy, do_clean, do_noisy, dq_clean, dk_clean, dv_clean, dq_noisy, dk_noisy, dv_noisy,
+                  workspace, workspace_bytes, cuda_stream);
+}
+
+int bdlm_doc_table(const int32_t* cu_seqlens, int32_t n_docs, int32_t L, int32_t* table, void* cuda_stream) {
+  if (n_docs <= 0 || L <= 0 || L > (1 << 30) || cu_seqlens == nullptr || table == nullptr) return BDLM_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(cu_seqlens) & 3u) || (reinterpret_cast<uintptr_t>(table) & 7u)) return BDLM_ERR_INVALID_ARG;
+  const cudaError_t e = launch_doc_table(cu_seqlens, n_docs, L, reinterpret_cast<int2*>(table), static_cast<cudaStream_t>(cuda_stream));
+  return e == cudaSuccess ? BDLM_OK : BDLM_ERR_CUDA;
+}
+
+int bdlm_attn_fwd_docs(const bdlm_params* p, const bdlm_packed_geometry* g, const bdlm_docs* docs,
+                       const void* q_clean, const void* k_clean, const void* v_clean,
+                       const void* q_noisy, const void* k_noisy, const void* v_noisy,
+                       void* o_clean, void* o_noisy, float* lse_clean, float* lse_noisy,
+                       void* cuda_stream) {
+  if (g == nullptr) return BDLM_ERR_INVALID_ARG;
+  const int rc = check_docs(g, docs);
+  if (rc != BDLM_OK) return rc;
+  return fwd_impl(p, g, docs, q_clean, k_clean, v_clean, q_noisy, k_noisy, v_noisy, o_clean, o_noisy,
+                  lse_clean, lse_noisy, cuda_stream);
+}
+
+int bdlm_attn_bwd_docs(const bdlm_params* p, const bdlm_packed_geometry* g, const bdlm_docs* docs,
+                       const void* q_clean, const void* k_clean, const void* v_clean,
+                       const void* q_noisy, const void* k_noisy, const void* v_noisy,
+                       const void* o_clean, const void* o_noisy,
+                       const float* lse_clean, const float* lse_noisy,
+                       const void* do_clean, const void* do_noisy,
+                       void* dq_clean, void* dk_clean, void* dv_clean,
+                       void* dq_noisy, void* dk_noisy, void* dv_noisy,
+                       void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  if (g == nullptr) return BDLM_ERR_INVALID_ARG;
+  const int rc = check_docs(g, docs);
+  if (rc != BDLM_OK) return rc;
+  return bwd_impl(p, g, docs, q_clean, k_clean, v_clean, q_noisy, k_noisy, v_noisy, o_clean, o_noisy, lse_clean,
                   lse_noisy, do_clean, do_noisy, dq_clean, dk_clean, dv_clean, dq_noisy, dk_noisy, dv_noisy,
                   workspace, workspace_bytes, cuda_stream);
 }

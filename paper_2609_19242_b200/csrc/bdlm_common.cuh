@@ -32,6 +32,11 @@ struct KArgs {
   int kv_chunk_len;
   const int* kv_chunk_pos;
   const int* kv_pos_chunk;
+  // Packed documents: docs[p] = first position and end of the document that holds position p, p = 0 .. L (p, p where none
+  // does); nullptr: the whole sequence is one.  doc_max, doc_pairs: what the rules on sizes know of them.
+  const int2* docs;
+  int doc_max;
+  double doc_pairs;
   float scale;        // q.k multiplier (1/sqrt(d) by default)
   float scale_log2;   // scale * log2(e): scores are exponentiated with exp2
   int mode;           // clean_mask_mode
@@ -86,10 +91,15 @@ __device__ __forceinline__ int first_block_prefix_gt(const KArgs& a, int x) {
   return lo;
 }
 
+// First position and end of the document that holds position p.
+__device__ __forceinline__ int2 doc_at(const KArgs& a, int p) { return __ldg(a.docs + max(0, min(p, a.L))); }
+
 // Visible key interval [lo, hi) of query row i (stream qs) inside key stream ks
 // (section 3.2: clean row -> clean keys 0..position; noisy row -> the clean keys before its block's
 // prefix and the noisy keys of its own block).  Every row's visible set per key stream is one interval.
 // Sliding-window layers: a clean key j is visible to a token at position p only if p - j < window.
+// Packed documents: only keys of the same document; a noisy block belongs to the document of the position it starts at.  Both
+// ends of the intervals stay monotone along the rows, which is all that the tile schedules rely on.
 __device__ __forceinline__ void visible_interval(const KArgs& a, int qs, int ks, int i, int& lo, int& hi) {
   const int M = a.M;
   if (ks == NOISY) {
@@ -108,6 +118,11 @@ __device__ __forceinline__ void visible_interval(const KArgs& a, int qs, int ks,
   }
   lo = a.kv_begin;
   if (a.window > 0) lo = max(lo, pos - a.window + 1);
+  if (a.docs != nullptr) {
+    const int2 doc = doc_at(a, qs == CLEAN ? pos : lim);
+    lo = max(lo, doc.x);
+    if (qs == CLEAN) lim = min(lim, doc.y);
+  }
   hi = min(a.kv_end, lim);
 }
 
@@ -119,6 +134,11 @@ __device__ __forceinline__ void visible_queries_of_clean_key(const KArgs& a, int
     const int p_lo = (a.mode == 0) ? j : (j / M) * M;
     lo = max(0, p_lo - a.cq_pos0);
     hi = (W > 0) ? min(a.Lqc, j + W - a.cq_pos0) : a.Lqc;
+    if (a.docs != nullptr) {
+      const int2 doc = doc_at(a, min(j, a.L - 1));
+      lo = max(lo, doc.x - a.cq_pos0);
+      hi = min(hi, doc.y - a.cq_pos0);
+    }
     hi = max(hi, 0);
   } else {
     lo = first_block_prefix_gt(a, j) * M;
@@ -128,6 +148,7 @@ __device__ __forceinline__ void visible_queries_of_clean_key(const KArgs& a, int
       const int b1 = first_block_prefix_gt(a, j + W - M);
       hi = (b1 >= a.nb) ? a.Ln : b1 * M + min(M, max(0, W + j - block_prefix(a, b1)));
     }
+    if (a.docs != nullptr) hi = min(hi, first_block_prefix_gt(a, doc_at(a, min(j, a.L - 1)).y - 1) * M);
   }
 }
 
@@ -195,7 +216,8 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 
 // The call as the rules on sizes see it.
 inline BwdSizes bwd_sizes(const KArgs& a) {
-  return {a.batch, a.L, a.q[CLEAN] != nullptr ? a.Lqc : 0, a.cq_pos0, a.q[NOISY] != nullptr ? a.Ln : 0, a.Hkv, a.G, a.window, a.kv_chunk_len};
+  return {a.batch, a.L, a.q[CLEAN] != nullptr ? a.Lqc : 0, a.cq_pos0, a.q[NOISY] != nullptr ? a.Ln : 0, a.Hkv, a.G, a.window, a.kv_chunk_len,
+          a.docs != nullptr ? a.doc_max : 0, a.docs != nullptr ? a.doc_pairs : 0};
 }
 
 // Launchers (host).  Each enqueues on `st` and returns the launch's cudaError_t.
@@ -203,6 +225,8 @@ cudaError_t launch_portable_fwd(const KArgs& a, cudaStream_t st);
 cudaError_t launch_portable_bwd(const KArgs& a, int passes, cudaStream_t st);
 // D rows of both query streams; with zero_dq the fused backward's accumulators a.dq32 are cleared in the same launch.
 cudaError_t launch_bwd_prepare(const KArgs& a, float* dsum_clean, float* dsum_noisy, bool zero_dq, cudaStream_t st);
+// The table of documents (bdlm_doc_table).
+cudaError_t launch_doc_table(const int* cu_seqlens, int n_docs, int L, int2* table, cudaStream_t st);
 cudaError_t launch_merge(int n, int batch, int L, int H, int d, const void* const* o_parts,
                          const float* const* lse_parts, int dtype, void* o_out, float* lse_out,
                          cudaStream_t st);

@@ -9,6 +9,8 @@ namespace bdlm {
 struct BwdSizes {
   int batch, L, Lqc, cq_pos0, Ln;   // clean keys, clean query rows (0: none) from this position on, noisy rows (0: none)
   int Hkv, G, window, kv_chunk_len;
+  int doc_max = 0;        // packed documents: tokens of the longest (0: none)
+  double doc_pairs = 0;   // and the sum of n (n + 1) / 2 over their lengths n (0: not known)
 };
 
 // Whether the units of a launch start tile-major (see TileGrid).  A stack (one head of one batch element and stream; ny nz of
@@ -48,7 +50,8 @@ constexpr double ORDER_RATIO = 5;   // one CTA per tile: 10 SMs > ny nz (nx + 1)
 // 20480 rows, H = 64 / 8 7814 / 8316).
 inline bool pairs_tile_major_pay(const BwdSizes& z, int sms, bool dq) {
   const int keys = dq && z.Hkv * z.G * z.batch >= 32 ? std::max(z.L, z.Ln) : z.L, nx = (keys + 255) / 256;
-  const double band = z.window > 0 ? z.window / 256.0 + 1 : nx, heavy = band < nx ? band : nx;
+  const int W = z.doc_max > 0 && (z.window == 0 || z.doc_max < z.window) ? z.doc_max : z.window;
+  const double band = W > 0 ? W / 256.0 + 1 : nx, heavy = band < nx ? band : nx;
   return tile_major_pays(nx, z.Hkv, 2 * z.batch, heavy, sms / 2, !dq ? 20.0 / 3 : heavy < nx ? 4.2 : 6);
 }
 
@@ -77,13 +80,14 @@ constexpr int TILE_KEYS = 128, STEP_ROWS = 64;
 constexpr double MIN_HEAVY = 24, SPLIT_2 = 1.2, SPLIT_4 = 3.0;
 struct KeyLoad { double heavy, mean, total; };   // steps of STEP_ROWS query rows: of the first clean key tile, per SM, of all clean key tiles of a KV head
 inline KeyLoad key_load(const BwdSizes& z, int sms) {
-  const double W = z.window > 0 ? z.window : 0;
+  // documents limit what a key sees as a window does; the keys that a query sees on average follow from their lengths
+  const double W = z.doc_max > 0 ? (z.window > 0 ? std::min(z.window, z.doc_max) : z.doc_max) : z.window > 0 ? z.window : 0;
   double heavy = 0, total = 0;
   for (int noisy = 0; noisy <= 1; ++noisy) {
     const int rows = noisy ? z.Ln : z.Lqc;
     if (rows == 0) continue;
     const double nq = (rows + STEP_ROWS - 1) / STEP_ROWS;
-    const double seen = noisy ? 0.5 * z.L : z.cq_pos0 + 0.5 * z.Lqc;   // keys a query sees on average
+    const double seen = z.doc_pairs > 0 ? z.doc_pairs / z.L : noisy ? 0.5 * z.L : z.cq_pos0 + 0.5 * z.Lqc;   // keys a query sees on average
     heavy += W > 0 ? std::min(nq, (W + TILE_KEYS) / STEP_ROWS + 1) : nq;
     total += nq * ((W > 0 ? std::min(W, seen) : seen) / TILE_KEYS + 1);
   }

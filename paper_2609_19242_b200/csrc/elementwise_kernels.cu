@@ -191,7 +191,28 @@ __global__ void __launch_bounds__(256) bwd_prepare_kernel(const PrepArgs pa) {
   }
 }
 
+// One thread per position: the last document that starts at or before it, by bisection of the starts.  Written once for a
+// packed batch and read by every layer's kernels, one 8-byte load per row, where bisecting in them would put ten dependent
+// loads before every unit's first tile.
+__global__ void __launch_bounds__(256) doc_table_kernel(const int* __restrict__ cu, int n, int L, int2* __restrict__ table) {
+  const int64_t p = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (p > L) return;
+  int lo = 0, hi = n;   // cu[lo] <= p < cu[hi], as far as there are such
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (cu[mid] <= p) lo = mid; else hi = mid;
+  }
+  // (bad entries give wrong documents, never positions outside [0, L])
+  const int a = max(0, min(cu[lo], L)), z = max(0, min(cu[lo + 1], L));
+  table[p] = a <= p && p < z ? make_int2(a, z) : make_int2((int)p, (int)p);
+}
+
 }  // namespace
+
+cudaError_t launch_doc_table(const int* cu_seqlens, int n_docs, int L, int2* table, cudaStream_t st) {
+  doc_table_kernel<<<(unsigned)(((int64_t)L + 256) / 256), 256, 0, st>>>(cu_seqlens, n_docs, L, table);
+  return cudaGetLastError();
+}
 
 cudaError_t launch_merge(int n, int batch, int L, int H, int d, const void* const* o_parts,
                          const float* const* lse_parts, int dtype, void* o_out, float* lse_out,

@@ -1,0 +1,269 @@
+"""Attention over packed documents (a table of documents with the packed form) against the oracle run on each document by
+itself, through the C ABI, both kernel families and both backward paths.
+
+Tolerances: parity_util's for outputs; gradients are compared document by document, so that a wrong short one cannot hide
+beside long ones.  Besides TOL_GRAD of the document's gradient they allow what D = dO . O, taken from the bf16 output, is off by:
+|dD_i| <= 2^-8 |dO_i| |O_i| (twice the rounding) enters dQ_i as scale dD_i sum_j P_ij k_j, and dK as scale P^T (dD q), whose norm is at most
+scale sqrt(n) |dD q|_F because no row of P sums to more than one and no column of n rows to more than n."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import bdlm_oracle as orc
+from paper_2609_19242_b200 import binding, synth
+
+import parity_util as pu
+
+pytestmark = pytest.mark.gpu
+
+AUTO, PORTABLE = binding.IMPL_AUTO, binding.IMPL_PORTABLE
+CLEAN_NAMES = ("q_clean", "k_clean", "v_clean", "do_clean")
+NOISY_NAMES = ("q_noisy", "k_noisy", "v_noisy", "do_noisy")
+
+
+def _inputs(L, Lq, Ln, H, Hkv, d, batch=1, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    mk = lambda rows, heads, s: (torch.randn(batch, rows, heads, d, generator=g) * s).to(torch.bfloat16) if rows else None
+    t = {"q_clean": mk(Lq, H, 1.0), "k_clean": mk(L, Hkv, 1.0), "v_clean": mk(L, Hkv, 1.0), "do_clean": mk(Lq, H, 1.0),
+         "q_noisy": mk(Ln, H, 1.0), "k_noisy": mk(Ln, Hkv, 1.0), "v_noisy": mk(Ln, Hkv, 1.0), "do_noisy": mk(Ln, H, 1.0)}
+    return t, {k: None if v is None else v.cuda() for k, v in t.items()}, {k: None if v is None else synth.to_f64(v) for k, v in t.items()}
+
+
+def _run(g, M, docs, prefix=None, pos0=0, window=0, mode=0, impl=AUTO, single_pass=None):
+    kw = dict(block_prefix=None if prefix is None else torch.tensor(prefix, dtype=torch.int32, device="cuda"), clean_q_pos0=pos0,
+              impl=impl, window=window, clean_mask_mode=mode, docs=docs)
+    qkv = [g[n] for n in ("q_clean", "k_clean", "v_clean", "q_noisy", "k_noisy", "v_noisy")]
+    out = binding.bdlm_attn_fwd_packed(*qkv, M, **kw)
+    grads = binding.bdlm_attn_bwd_packed(*qkv, *out, g["do_clean"], g["do_noisy"], M, single_pass=single_pass, **kw)
+    torch.cuda.synchronize()
+    assert binding.bdlm_get_device_status() == 0
+    return out, grads
+
+
+def _norms(t):
+    return np.sqrt((t ** 2).sum(axis=-1))
+
+
+def _check(lens, M=1, H=2, Hkv=1, d=128, noisy=None, pos0=0, Lq=None, window=0, mode=0, impl=AUTO, single_pass=None, batch=1, before=0,
+           after=0, seed=0):
+    """noisy: None, "all" (every whole block of every document) or a sorted list of prefixes.  before, after: positions of no document."""
+    cu = np.cumsum([before] + list(lens))
+    L = int(cu[-1]) + after
+    Lq = L - pos0 if Lq is None else Lq
+    prefix = noisy
+    if noisy == "all":
+        prefix = [a + b * M for a, n in zip(cu, lens) for b in range(n // M)]
+    nb = 0 if prefix is None else len(prefix)
+    t, g, x = _inputs(L, Lq, nb * M, H, Hkv, d, batch, seed)
+    docs = binding.bdlm_doc_table(torch.tensor(cu, dtype=torch.int32), L)
+    out, grads = _run(g, M, docs, prefix, pos0, window, mode, impl, single_pass)
+    got = {n: None if v is None else synth.to_f64(v) for n, v in
+           zip(("o_clean", "lse_clean", "o_noisy", "lse_noisy", "dq_clean", "dk_clean", "dv_clean", "dq_noisy", "dk_noisy", "dv_noisy"), (*out, *grads))}
+    scale, G = 1.0 / np.sqrt(d), H // Hkv
+    seen_keys = np.zeros(L, dtype=bool)
+    seen_blocks = np.zeros(nb, dtype=bool)
+    for a, n in zip(cu, lens):
+        z = a + n
+        if n == 0:
+            continue
+        seen_keys[a:z] = True
+        r0, r1 = max(a, pos0), min(z, pos0 + Lq)                 # this document's clean queries
+        blocks = [b for b in range(nb) if a <= prefix[b] < z]
+        seen_blocks[blocks] = True
+        rows_n = np.concatenate([np.arange(b * M, (b + 1) * M) for b in blocks]) if blocks else np.zeros(0, dtype=int)
+        rows_c = np.arange(r0 - pos0, r1 - pos0) if r1 > r0 else np.zeros(0, dtype=int)
+        part = lambda name, rows: x[name][:, rows] if len(rows) else None
+        kn, vn = part("k_noisy", rows_n), part("v_noisy", rows_n)
+        if kn is None:
+            kn = vn = np.zeros((batch, 0, Hkv, d))
+        ref = orc.attn_packed(part("q_clean", rows_c), x["k_clean"][:, a:z], x["v_clean"][:, a:z], part("q_noisy", rows_n), kn, vn, M,
+                              do_clean=part("do_clean", rows_c), do_noisy=part("do_noisy", rows_n),
+                              block_prefix=[prefix[b] - a for b in blocks], clean_q_pos0=r0 - a, window=window, clean_mask_mode=mode)
+        d_q = {}   # |dD_i| |q_i| bounds per stream, for dK
+        for s, rows in (("clean", rows_c), ("noisy", rows_n)):
+            if not len(rows):
+                continue
+            o, lse = got["o_" + s][:, rows], got["lse_" + s][:, :, rows]
+            assert np.abs(o - ref["o_" + s]).max() <= pu.TOL_O * max(1.0, np.abs(ref["o_" + s]).max()), (s, a, n)
+            assert np.abs(lse - ref["lse_" + s]).max() <= pu.TOL_LSE, (s, a, n)
+            do = x["do_" + s][:, rows]
+            dD = 2.0 ** -8 * _norms(do) * _norms(ref["o_" + s])   # [batch, rows, H]
+            kmax = max(_norms(x["k_clean"][:, a:z]).max(), _norms(kn).max() if kn.shape[1] else 0.0)
+            off = np.sqrt(((scale * dD * kmax) ** 2).sum())
+            err = np.linalg.norm(got["dq_" + s][:, rows] - ref["dq_" + s])
+            assert err <= pu.TOL_GRAD * np.linalg.norm(ref["dq_" + s]) + off, (s, a, n, err, off)
+            d_q[s] = (dD * _norms(x["q_" + s][:, rows])) ** 2
+        n_rows = (len(rows_c) + len(rows_n)) * G
+        slack = scale * np.sqrt(max(n_rows, 1)) * np.sqrt(sum(v.sum() for v in d_q.values()))
+        if not d_q:
+            ref.update(dk_clean=np.zeros((batch, n, Hkv, d)), dv_clean=np.zeros((batch, n, Hkv, d)))
+        for name, rows in (("clean", np.arange(a, z)), ("noisy", rows_n)):
+            if not len(rows):
+                continue
+            for which, off in (("dk_", slack), ("dv_", 0.0)):
+                have, want = got[which + name][:, rows], ref[which + name]
+                err = np.linalg.norm(have - want)
+                assert err <= pu.TOL_GRAD * np.linalg.norm(want) + off, (which + name, a, n, err, off)
+    # positions of no document see nothing and are seen by nothing; a block at one of them sees itself only
+    if Lq:
+        rows = np.array([i for i in range(Lq) if not seen_keys[pos0 + i]], dtype=int)
+        assert (got["o_clean"][:, rows] == 0).all() and np.isneginf(got["lse_clean"][:, :, rows]).all() and (got["dq_clean"][:, rows] == 0).all()
+    assert (got["dk_clean"][:, ~seen_keys] == 0).all() and (got["dv_clean"][:, ~seen_keys] == 0).all()
+    for b in np.nonzero(~seen_blocks)[0]:
+        rows = np.arange(b * M, (b + 1) * M)
+        ref = orc.attn_packed(None, np.zeros((batch, 0, Hkv, d)), np.zeros((batch, 0, Hkv, d)), x["q_noisy"][:, rows], x["k_noisy"][:, rows],
+                              x["v_noisy"][:, rows], M, block_prefix=[0])
+        assert np.abs(got["o_noisy"][:, rows] - ref["o_noisy"]).max() <= pu.TOL_O * max(1.0, np.abs(ref["o_noisy"]).max())
+    for v in got.values():
+        assert v is None or not np.isnan(v).any()
+    return out, grads
+
+
+PATHS = [(AUTO, True), (AUTO, False), (PORTABLE, False)]
+
+
+@pytest.mark.parametrize("impl,single", PATHS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens", [[1], [5], [128], [1, 1, 1], [127, 1, 129], [100, 1, 27, 128], [300, 2, 40, 0, 90], [64] * 9, [383, 257, 1]],
+                         ids=lambda l: "-".join(map(str, l)))
+def test_prompts_of_different_lengths(lens, d, impl, single):
+    _check(lens, d=d, impl=impl, single_pass=single)
+
+
+@pytest.mark.parametrize("impl,single", PATHS)
+@pytest.mark.parametrize("H,Hkv", [(1, 1), (3, 1), (4, 2), (6, 2), (8, 1)])
+def test_grouped_heads(H, Hkv, impl, single):
+    _check([200, 33, 150], H=H, Hkv=Hkv, impl=impl, single_pass=single)
+    _check([200, 33, 150], H=H, Hkv=Hkv, d=64, impl=impl, single_pass=single, batch=2)
+
+
+@pytest.mark.parametrize("impl,single", PATHS)
+@pytest.mark.parametrize("M,lens", [(16, [48, 16, 160, 96]), (32, [320, 32, 64, 128]), (40, [200, 40, 120]), (4, [100, 8, 60]), (128, [256, 128])])
+def test_both_streams_over_documents_of_whole_blocks(M, lens, impl, single):
+    _check(lens, M=M, H=4, Hkv=2, noisy="all", impl=impl, single_pass=single)
+    _check(lens, M=M, H=3, Hkv=1, d=64, noisy="all", mode=1, impl=impl, single_pass=single)
+
+
+@pytest.mark.parametrize("impl,single", PATHS)
+def test_sampled_blocks(impl, single):
+    """Anchors at a document's first and last positions, repeated ones, and past all documents."""
+    _check([300, 77, 200], M=16, noisy=[0, 0, 1, 150, 299, 300, 301, 376, 377, 420, 576], pos0=0, impl=impl, single_pass=single)
+    _check([300, 77, 200], M=16, noisy=[5, 290, 300, 377, 570, 577], Lq=0, impl=impl, single_pass=single)
+    _check([64, 64], M=8, noisy=[3, 64, 127, 128, 128], Lq=0, impl=impl, single_pass=single)
+
+
+@pytest.mark.parametrize("impl,single", PATHS)
+def test_sliding_window(impl, single):
+    for window in (1, 33, 150, 1000):
+        _check([260, 40, 300], window=window, impl=impl, single_pass=single)
+    _check([256, 64, 320], M=32, noisy="all", window=100, impl=impl, single_pass=single)
+
+
+@pytest.mark.parametrize("impl,single", PATHS)
+def test_a_run_of_queries_at_an_offset(impl, single):
+    """A rank's piece of the packed sequence: it begins and ends inside documents, and misses others."""
+    _check([150, 100, 260, 90], pos0=200, Lq=200, impl=impl, single_pass=single)
+    _check([150, 100, 260, 90], pos0=330, Lq=1, impl=impl, single_pass=single)
+    _check([150, 100, 260, 90], pos0=250, Lq=260, M=10, noisy=[0, 100, 160, 260, 500], impl=impl, single_pass=single)
+
+
+@pytest.mark.parametrize("impl,single", PATHS)
+def test_positions_of_no_document(impl, single):
+    _check([100, 200], before=70, after=130, impl=impl, single_pass=single)
+    _check([100, 1], after=300, impl=impl, single_pass=single)
+    _check([96, 64], M=16, before=16, after=32, noisy=[0, 16, 64, 112, 160, 176, 180], impl=impl, single_pass=single)
+
+
+def test_long_documents_on_pairs_of_ctas_and_clusters():
+    """Sizes at which the backward shares key tiles among CTAs, or takes two at a time, whatever the documents are."""
+    _check([700, 1300, 48], H=8, Hkv=1, single_pass=True)          # few tiles, many steps: clusters share them
+    t, g, _ = _inputs(6144, 6144, 0, 32, 8, 128)
+    lens = [6000, 144]
+    docs = binding.bdlm_doc_table([0, 6000, 6144])
+    out, grads = _run(g, 1, docs)
+    # the documents by themselves, through the plain packed form
+    for a, z in ((0, 6000), (6000, 6144)):
+        part = {k: None if v is None else v[:, a:z].contiguous() for k, v in g.items()}
+        qkv = [part[n] for n in ("q_clean", "k_clean", "v_clean")] + [None] * 3
+        o, lse, _, _ = binding.bdlm_attn_fwd_packed(*qkv, 1)
+        # the same products; a document that does not begin on a tile's first row is cut into tiles elsewhere
+        assert float((out[0][:, a:z].float() - o.float()).abs().max()) <= pu.TOL_O
+        assert float((out[1][:, :, a:z] - lse).abs().max()) <= pu.TOL_LSE
+        ref = binding.bdlm_attn_bwd_packed(*qkv, o, lse, None, None, part["do_clean"], None, 1, single_pass=False)
+        for have, want in zip(grads[:3], ref[:3]):
+            assert pu.rel_l2(synth.to_f64(have[:, a:z]), synth.to_f64(want)) <= 1e-2
+
+
+def test_one_document_is_the_plain_form_bit_for_bit():
+    t, g, _ = _inputs(700, 700, 0, 4, 2, 128, batch=2)
+    docs = binding.bdlm_doc_table([0, 700])
+    out, grads = _run(g, 1, docs, single_pass=False)
+    plain, pgrads = _run(g, 1, None, single_pass=False)
+    for a, b in zip((*out[:2], *grads[:3]), (*plain[:2], *pgrads[:3])):
+        assert torch.equal(a, b)
+
+
+def test_neighbours_have_no_effect():
+    """Other values in the other documents change nothing, large ones included."""
+    t, g, _ = _inputs(900, 900, 0, 4, 2, 128)
+    docs = binding.bdlm_doc_table([0, 250, 600, 900])
+    out, grads = _run(g, 1, docs, single_pass=False)
+    for k in CLEAN_NAMES:
+        g[k][:, :250] *= 1000.0
+        g[k][:, 600:] = 65000.0
+    out2, grads2 = _run(g, 1, docs, single_pass=False)
+    at = slice(250, 600)
+    assert torch.equal(out[0][:, at], out2[0][:, at]) and torch.equal(out[1][:, :, at], out2[1][:, :, at])
+    for a, b in zip(grads[:3], grads2[:3]):
+        assert torch.equal(a[:, at], b[:, at])
+
+
+def test_reproducible_two_pass_gradients_and_capture():
+    t, g, _ = _inputs(640, 640, 0, 4, 2, 64)
+    docs = binding.bdlm_doc_table([0, 100, 101, 400, 640])
+    want, wgrads = _run(g, 1, docs, single_pass=False)
+    graph = torch.cuda.CUDAGraph()
+    qkv = [g[n] for n in ("q_clean", "k_clean", "v_clean")] + [None] * 3
+    with torch.cuda.graph(graph):
+        out = binding.bdlm_attn_fwd_packed(*qkv, 1, docs=docs)
+        grads = binding.bdlm_attn_bwd_packed(*qkv, *out, g["do_clean"], None, 1, docs=docs, single_pass=False)
+    for _ in range(2):
+        for t in (*out[:2], *grads[:3]):
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip((*out[:2], *grads[:3]), (*want[:2], *wgrads[:3])):
+            assert torch.equal(a, b)
+
+
+def test_table_of_documents():
+    for cu, L in (([0, 4, 4, 9], 9), ([2, 5, 6], 8), ([0, 1], 1), ([3, 3, 3], 5)):
+        table = binding.bdlm_doc_table(torch.tensor(cu, dtype=torch.int32, device="cuda"), L)
+        want = [[p, p] for p in range(L + 1)]
+        for a, z in zip(cu, cu[1:]):
+            for p in range(a, z):
+                want[p] = [a, z]
+        assert table.table.cpu().tolist() == want
+        assert table.max_len == max(z - a for a, z in zip(cu, cu[1:]))
+
+
+def test_wrong_tables_stay_inside_the_tensors():
+    """The library does not validate the entries on the device: wrong ones give wrong documents inside [0, L]."""
+    cu = torch.tensor([50, 20, -7, 2 ** 31 - 1, 90], dtype=torch.int32, device="cuda")
+    table = torch.empty(65, 2, dtype=torch.int32, device="cuda")
+    assert binding.lib().bdlm_doc_table(cu.data_ptr(), 4, 64, table.data_ptr(), binding._stream()) == 0
+    assert int(table.min()) >= 0 and int(table.max()) <= 64
+
+
+def test_refusals():
+    t, g, _ = _inputs(256, 256, 0, 2, 1, 64)
+    qkv = [g[n] for n in ("q_clean", "k_clean", "v_clean")] + [None] * 3
+    for bad in ([0], [0, 5, 3], [-1, 4], [[0, 4]], torch.tensor([0.0, 4.0])):
+        with pytest.raises(ValueError):
+            binding.bdlm_doc_table(bad)
+    with pytest.raises(ValueError):
+        binding.bdlm_doc_table([0, 100], 50)
+    with pytest.raises(ValueError):
+        binding.bdlm_attn_fwd_packed(*qkv, 1, docs=binding.bdlm_doc_table([0, 255]))
+    with pytest.raises(ValueError):
+        binding.bdlm_attn_fwd_packed(*qkv, 1, docs=binding.bdlm_doc_table([0, 256]), kv_chunks=(128, [128, 0]))
