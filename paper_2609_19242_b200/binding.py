@@ -24,8 +24,11 @@ EXPORTS = ("bdlm_workspace_bytes", "bdlm_attn_fwd", "bdlm_attn_bwd", "bdlm_lse_m
            "bdlm_status_string", "bdlm_get_device_status", "bdlm_set_trace_buffer",
            "bdlm_attn_bwd_static_scratch", "bdlm_workspace_bytes_packed", "bdlm_attn_fwd_packed",
            "bdlm_attn_bwd_packed", "bdlm_selftest_wait_timeout", "bdlm_linear_ce_workspace_bytes",
-           "bdlm_linear_ce_fwd", "bdlm_linear_ce_bwd", "bdlm_doc_table", "bdlm_attn_fwd_docs", "bdlm_attn_bwd_docs")
+           "bdlm_linear_ce_fwd", "bdlm_linear_ce_bwd", "bdlm_doc_table", "bdlm_attn_fwd_docs", "bdlm_attn_bwd_docs",
+           "bdlm_norm_workspace_bytes", "bdlm_norm_fwd", "bdlm_norm_bwd")
 LCE_WS_FWD, LCE_WS_BWD, LCE_WS_FWD_LEAST, LCE_WS_BWD_LEAST = 0, 1, 2, 3
+NORM_LAYER, NORM_RMS, NORM_MAX_D = 0, 1, 16384
+DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 STATIC_SCRATCH_ROWS = 1 << 20
 TRACE_SLOTS = 256
 
@@ -59,6 +62,11 @@ class BdlmDocs(ctypes.Structure):
 class BdlmLceParams(ctypes.Structure):
     _fields_ = [("T", ctypes.c_int32), ("D", ctypes.c_int32), ("V", ctypes.c_int32), ("token_chunk", ctypes.c_int32),
                 ("grad_loss", ctypes.c_float), ("reserved", ctypes.c_int32 * 3)]
+
+
+class BdlmNormParams(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("D", ctypes.c_int32), ("dtype", ctypes.c_int32), ("wdtype", ctypes.c_int32),
+                ("kind", ctypes.c_int32), ("eps", ctypes.c_float), ("reserved", ctypes.c_int32 * 2)]
 
 
 _lib = None
@@ -111,6 +119,13 @@ def lib():
         L.bdlm_linear_ce_fwd.argtypes = [lp] + [vp] * 7 + [vp, ctypes.c_size_t, vp]
         L.bdlm_linear_ce_bwd.restype = ctypes.c_int
         L.bdlm_linear_ce_bwd.argtypes = [lp] + [vp] * 7 + [vp, ctypes.c_size_t, vp]
+        np_ = ctypes.POINTER(BdlmNormParams)
+        L.bdlm_norm_workspace_bytes.restype = ctypes.c_size_t
+        L.bdlm_norm_workspace_bytes.argtypes = [np_]
+        L.bdlm_norm_fwd.restype = ctypes.c_int
+        L.bdlm_norm_fwd.argtypes = [np_] + [vp] * 8 + [vp]
+        L.bdlm_norm_bwd.restype = ctypes.c_int
+        L.bdlm_norm_bwd.argtypes = [np_] + [vp] * 9 + [vp, ctypes.c_size_t, vp]
         L.bdlm_selftest_wait_timeout.restype = ctypes.c_int
         L.bdlm_selftest_wait_timeout.argtypes = [ctypes.c_int64, vp]
         _lib = L
@@ -526,4 +541,80 @@ def bdlm_linear_ce_bwd(h, w, labels, lse, token_weight=None, *, grad_loss=1.0, t
                                   _ptr(out[0]), _ptr(out[1]), _ptr(workspace), workspace.numel(), _stream())
     if rc != 0:
         raise BdlmError(rc, "bdlm_linear_ce_bwd")
+    return out
+
+
+# ------------------------------------------------------------------------------------------
+# normalisation (include/bdlm_norm.h)
+# ------------------------------------------------------------------------------------------
+def make_norm_params(T, D, dtype, wdtype, rms=False, eps=0.0) -> BdlmNormParams:
+    return BdlmNormParams(T, D, DTYPES[dtype], DTYPES[wdtype], NORM_RMS if rms else NORM_LAYER, eps)
+
+
+def bdlm_norm_workspace_bytes(params: BdlmNormParams) -> int:
+    return int(lib().bdlm_norm_workspace_bytes(ctypes.byref(params)))
+
+
+def _same(name, t, like, shape=None):
+    """`t` (if given) has the shape of `like` or `shape`, and lies on its device; the type too where no shape is given."""
+    if t is None:
+        return
+    if t.shape != (like.shape if shape is None else shape) or t.device != like.device or (shape is None and t.dtype != like.dtype):
+        raise ValueError(f"{name} does not match")
+
+
+def _row_stat(name, t, x):
+    _same(name, t, x, x.shape[:-1])
+    if t is not None and t.dtype != torch.float32:
+        raise ValueError(f"{name} must be fp32")
+
+
+def _check_weight(x, weight, **more):
+    for name, t in (("weight", weight), *more.items()):
+        _same(name, t, x, x.shape[-1:])
+        if t is not None and t.dtype != (x.dtype if weight is None else weight.dtype):
+            raise ValueError(f"{name} must be of the weight's type")
+
+
+def bdlm_norm_fwd(x, weight=None, bias=None, residual=None, *, eps=1e-5, rms=False, out=None):
+    """Layer norm (root-mean-square norm with `rms`) of h = x + residual along the last axis: x [..., D] bf16, fp16 or fp32,
+    weight and bias [D] of the same type or fp32.  Returns (y, h, mean, rstd): h is x itself where there is no residual, mean is None with
+    `rms`; mean and rstd [...] fp32 are what the backward reads.  `out` may supply those four."""
+    _on_current_device(x)
+    D = x.shape[-1]
+    _same("residual", residual, x)
+    _check_weight(x, weight, bias=bias)
+    p = make_norm_params(x.numel() // D if D else 0, D, x.dtype, x.dtype if weight is None else weight.dtype, rms, eps)
+    if out is None:
+        stat = lambda: torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+        out = (torch.empty_like(x), x if residual is None else torch.empty_like(x), None if rms else stat(), stat())
+    y, h, mean, rstd = out
+    _same("y", y, x), _same("h", h, x), _row_stat("mean", mean, x), _row_stat("rstd", rstd, x)
+    rc = lib().bdlm_norm_fwd(ctypes.byref(p), _ptr(x), _ptr(residual), _ptr(weight), _ptr(bias), _ptr(y),
+                             None if residual is None else _ptr(h), _ptr(mean), _ptr(rstd), _stream())
+    if rc != 0:
+        raise BdlmError(rc, "bdlm_norm_fwd")
+    return out
+
+
+def bdlm_norm_bwd(dy, h, weight, mean, rstd, *, dh=None, bias=False, rms=False, out=None, workspace=None):
+    """Backward: dy the gradient of y, dh (optional) the gradient that reaches h along the residual path; h, mean and rstd as the
+    forward returned them.  Returns (dx, dweight, dbias): dx is the gradient of x and of the residual, dweight is None without a
+    weight, dbias unless `bias`."""
+    _on_current_device(h)
+    D = h.shape[-1]
+    _same("dy", dy, h), _same("dh", dh, h), _row_stat("mean", mean, h), _row_stat("rstd", rstd, h)
+    _check_weight(h, weight)
+    p = make_norm_params(h.numel() // D if D else 0, D, h.dtype, h.dtype if weight is None else weight.dtype, rms)
+    if out is None:
+        out = (torch.empty_like(h), None if weight is None else torch.empty_like(weight),
+               torch.empty_like(weight) if bias and weight is not None else None)
+    dx, dw, db = out
+    _same("dx", dx, h), _check_weight(h, weight, dweight=dw, dbias=db)
+    if workspace is None and (dw is not None or db is not None):
+        workspace = torch.empty(max(bdlm_norm_workspace_bytes(p), 16), dtype=torch.uint8, device=h.device)
+    rc = lib().bdlm_norm_bwd(ctypes.byref(p), _ptr(dy), _ptr(h), _ptr(weight), _ptr(mean), _ptr(rstd), _ptr(dh), _ptr(dx),
+                             _ptr(dw), _ptr(db), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream())
+    if rc != 0:
+        raise BdlmError(rc, "bdlm_norm_bwd")
     return out
