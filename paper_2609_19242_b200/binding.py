@@ -25,7 +25,8 @@ EXPORTS = ("bdlm_workspace_bytes", "bdlm_attn_fwd", "bdlm_attn_bwd", "bdlm_lse_m
            "bdlm_attn_bwd_static_scratch", "bdlm_workspace_bytes_packed", "bdlm_attn_fwd_packed",
            "bdlm_attn_bwd_packed", "bdlm_selftest_wait_timeout", "bdlm_linear_ce_workspace_bytes",
            "bdlm_linear_ce_fwd", "bdlm_linear_ce_bwd", "bdlm_doc_table", "bdlm_attn_fwd_docs", "bdlm_attn_bwd_docs",
-           "bdlm_norm_workspace_bytes", "bdlm_norm_fwd", "bdlm_norm_bwd")
+           "bdlm_norm_workspace_bytes", "bdlm_norm_fwd", "bdlm_norm_bwd", "bdlm_embed_workspace_bytes", "bdlm_embed_fwd",
+           "bdlm_embed_bwd")
 LCE_WS_FWD, LCE_WS_BWD, LCE_WS_FWD_LEAST, LCE_WS_BWD_LEAST = 0, 1, 2, 3
 NORM_LAYER, NORM_RMS, NORM_MAX_D = 0, 1, 16384
 DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
@@ -67,6 +68,11 @@ class BdlmLceParams(ctypes.Structure):
 class BdlmNormParams(ctypes.Structure):
     _fields_ = [("T", ctypes.c_int32), ("D", ctypes.c_int32), ("dtype", ctypes.c_int32), ("wdtype", ctypes.c_int32),
                 ("kind", ctypes.c_int32), ("eps", ctypes.c_float), ("reserved", ctypes.c_int32 * 2)]
+
+
+class BdlmEmbedParams(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("D", ctypes.c_int32), ("V", ctypes.c_int32), ("table_dtype", ctypes.c_int32),
+                ("out_dtype", ctypes.c_int32), ("scale", ctypes.c_float), ("accumulate", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 _lib = None
@@ -119,13 +125,19 @@ def lib():
         L.bdlm_linear_ce_fwd.argtypes = [lp] + [vp] * 7 + [vp, ctypes.c_size_t, vp]
         L.bdlm_linear_ce_bwd.restype = ctypes.c_int
         L.bdlm_linear_ce_bwd.argtypes = [lp] + [vp] * 7 + [vp, ctypes.c_size_t, vp]
-        np_ = ctypes.POINTER(BdlmNormParams)
+        np_, ep = ctypes.POINTER(BdlmNormParams), ctypes.POINTER(BdlmEmbedParams)
         L.bdlm_norm_workspace_bytes.restype = ctypes.c_size_t
         L.bdlm_norm_workspace_bytes.argtypes = [np_]
         L.bdlm_norm_fwd.restype = ctypes.c_int
         L.bdlm_norm_fwd.argtypes = [np_] + [vp] * 8 + [vp]
         L.bdlm_norm_bwd.restype = ctypes.c_int
         L.bdlm_norm_bwd.argtypes = [np_] + [vp] * 9 + [vp, ctypes.c_size_t, vp]
+        L.bdlm_embed_workspace_bytes.restype = ctypes.c_size_t
+        L.bdlm_embed_workspace_bytes.argtypes = [ep]
+        L.bdlm_embed_fwd.restype = ctypes.c_int
+        L.bdlm_embed_fwd.argtypes = [ep] + [vp] * 3 + [vp]
+        L.bdlm_embed_bwd.restype = ctypes.c_int
+        L.bdlm_embed_bwd.argtypes = [ep] + [vp] * 3 + [vp, ctypes.c_size_t, vp]
         L.bdlm_selftest_wait_timeout.restype = ctypes.c_int
         L.bdlm_selftest_wait_timeout.argtypes = [ctypes.c_int64, vp]
         _lib = L
@@ -617,4 +629,53 @@ def bdlm_norm_bwd(dy, h, weight, mean, rstd, *, dh=None, bias=False, rms=False, 
                              _ptr(dw), _ptr(db), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream())
     if rc != 0:
         raise BdlmError(rc, "bdlm_norm_bwd")
+    return out
+
+
+# ------------------------------------------------------------------------------------------
+# token embedding (include/bdlm_embed.h)
+# ------------------------------------------------------------------------------------------
+def make_embed_params(T, D, V, table_dtype, out_dtype, scale=1.0, accumulate=False) -> BdlmEmbedParams:
+    return BdlmEmbedParams(T, D, V, DTYPES[table_dtype], DTYPES[out_dtype], scale, 1 if accumulate else 0)
+
+
+def bdlm_embed_workspace_bytes(params: BdlmEmbedParams) -> int:
+    return int(lib().bdlm_embed_workspace_bytes(ctypes.byref(params)))
+
+
+def bdlm_embed_fwd(table, ids, *, scale=1.0, dtype=None, out=None):
+    """Rows of table [V, D] for ids [...] int32 (outside [0, V): padding, a row of zeros), times `scale`.  Returns [..., D] of
+    `dtype`: the table's (default), or any of bf16, fp16 and fp32 for an fp32 table."""
+    _on_current_device(table)
+    V, D = table.shape
+    if ids.dtype != torch.int32 or ids.device != table.device:
+        raise ValueError("ids must be int32, on the table's device")
+    if out is None:
+        out = torch.empty(*ids.shape, D, dtype=table.dtype if dtype is None else dtype, device=table.device)
+    _same("out", out, table, (*ids.shape, D))
+    p = make_embed_params(ids.numel(), D, V, table.dtype, out.dtype, scale)
+    rc = lib().bdlm_embed_fwd(ctypes.byref(p), _ptr(table), _ptr(ids), _ptr(out), _stream())
+    if rc != 0:
+        raise BdlmError(rc, "bdlm_embed_fwd")
+    return out
+
+
+def bdlm_embed_bwd(dout, ids, V, *, scale=1.0, dtype=None, accumulate=False, out=None, workspace=None):
+    """Gradient of the table [V, D] for dout [..., D], the gradient of bdlm_embed_fwd's result: of `dtype` (default: dout's;
+    fp32 goes with any).  With `accumulate` it is added to `out`."""
+    _on_current_device(dout)
+    D = dout.shape[-1]
+    if ids.dtype != torch.int32 or ids.device != dout.device or dout.shape[:-1] != ids.shape:
+        raise ValueError("ids must be int32, one per row of dout, on its device")
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs the gradient to add to (out)")
+        out = torch.empty(V, D, dtype=dout.dtype if dtype is None else dtype, device=dout.device)
+    _same("out", out, dout, (V, D))
+    p = make_embed_params(ids.numel(), D, V, out.dtype, dout.dtype, scale, accumulate)
+    if workspace is None:
+        workspace = torch.empty(max(bdlm_embed_workspace_bytes(p), 16), dtype=torch.uint8, device=dout.device)
+    rc = lib().bdlm_embed_bwd(ctypes.byref(p), _ptr(dout), _ptr(ids), _ptr(out), _ptr(workspace), workspace.numel(), _stream())
+    if rc != 0:
+        raise BdlmError(rc, "bdlm_embed_bwd")
     return out

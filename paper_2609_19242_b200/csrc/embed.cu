@@ -1,0 +1,465 @@
+// Token embedding (include/bdlm_embed.h): rows of the table looked up and scaled, and the table's gradient over sorted tokens.
+//
+// The lookup is a copy of T rows: 2 T D elements, bound by memory.
+//
+// The gradient has to read T D elements and write V D of them, most of the latter zeros (a batch holds a few thousand of
+// 128256 tokens).  Three launches, chained:
+//   sort    one cluster sorts (id, position) by id, a stable radix sort whose CTAs exchange their digits' counts through
+//           distributed shared memory; the pairs ping-pong through the workspace, which stays in L2
+//   sum     zeros the rows of tokens that do not occur -- it finds them in the ids themselves, so this runs beside the sort --
+//           and then, once the sort is done, sums the sorted tokens' rows in pieces of `piece` tokens.  A run of equal ids that
+//           lies inside a piece is finished there; of one that crosses into other pieces, each piece leaves an fp32 part.
+//   join    adds the parts of the runs that cross pieces (the mask token's run crosses thousands)
+// Every sum runs in the tokens' order inside a piece and over the pieces in order of eight interleaved shares, so it depends on
+// T only, not on how often a token occurs or where.
+#include <math.h>
+
+#include "../../include/bdlm_embed.h"
+#include "elem_common.cuh"
+
+namespace bdlm {
+namespace {
+
+__device__ __forceinline__ uint32_t ctas_of_cluster() { uint32_t n; asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(n)); return n; }
+__device__ __forceinline__ uint32_t cta_of_cluster() { uint32_t n; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(n)); return n; }
+// Also orders the CTAs' writes to global memory before the others' reads of it (release and acquire at cluster scope).
+__device__ __forceinline__ void whole_cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ int ld_cluster_int(const int* own, int rank) {
+  const uint32_t at = (uint32_t)__cvta_generic_to_shared(own);
+  int v;
+  asm volatile("{\n\t.reg .u32 a;\n\tmapa.shared::cluster.u32 a, %1, %2;\n\tld.shared::cluster.u32 %0, [a];\n\t}" : "=r"(v) : "r"(at), "r"(rank) : "memory");
+  return v;
+}
+__device__ __forceinline__ void wait_for_sort() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+// ------------------------------------------------------------------------------------------------ lookup
+// `tpr` threads (a power of two) share a row, four vectors of it in flight in each.
+template <class E, class O, int V>
+__global__ void __launch_bounds__(256) embed_fwd_kernel(const E* table, const int* ids, O* out, int T, int D, int vocab, int tpr, float scale) {
+  const int rows = 256 / tpr, lane = threadIdx.x % tpr;
+  const int64_t row = (int64_t)blockIdx.x * rows + threadIdx.x / tpr;
+  if (row >= T) return;
+  const int id = ids[row];
+  const bool real = id >= 0 && id < vocab;
+  const int nvec = D / V;
+  const E* src = table + (int64_t)(real ? id : 0) * D;
+  O* dst = out + row * D;
+  constexpr int U = 4;
+  for (int c0 = lane; c0 < nvec; c0 += U * tpr) {
+    Raw<E, V> r[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      r[u].clear();
+      if (real && c0 + u * tpr < nvec) r[u].load(src + (int64_t)(c0 + u * tpr) * V);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (c0 + u * tpr < nvec) {
+        float f[V];
+        Raw<O, V> o;
+        r[u].get(f);
+#pragma unroll
+        for (int e = 0; e < V; ++e) f[e] *= scale;
+        o.put(f);
+        o.store(dst + (int64_t)(c0 + u * tpr) * V);
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ sort
+constexpr int SORT_WARPS = 32, DIGIT_BITS = 9, BINS = 1 << DIGIT_BITS;
+constexpr int SORT_SMEM = (SORT_WARPS + 2) * BINS * (int)sizeof(int) + 32 * (int)sizeof(int);
+
+// Pairs (key, position), sorted by key with positions ascending among equal keys; key = id, or V where the id is no token.
+// A warp owns a run of `seg` consecutive pairs.  A pass counts each warp's digits, turns the counts into the places where
+// each warp's pairs of each digit begin (over the bins, then the CTAs, then the warps), and moves the pairs; equal digits
+// inside a group of 32 are ranked by a vote.  The last pass writes `sorted`.
+__global__ void __launch_bounds__(SORT_WARPS * 32) embed_sort_kernel(const int* ids, int T, int V, int passes, int bits, int2* sorted, int2* other) {
+  extern __shared__ int sm[];
+  int* hist = sm;                               // [warp][bin]
+  int* total = sm + SORT_WARPS * BINS;          // this CTA's count of each bin, read by the others
+  int* base = total + BINS;                     // where this CTA's pairs of each bin begin
+  int* scan = base + BINS;
+  let_next_start();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, bins = 1 << bits;
+  const int ctas = (int)ctas_of_cluster(), rank = (int)cta_of_cluster();
+  const int warps = ctas * SORT_WARPS;
+  const int64_t seg = (((int64_t)T + warps - 1) / warps + 31) / 32 * 32;
+  const int64_t first = min((int64_t)T, (int64_t)(rank * SORT_WARPS + warp) * seg), last = min((int64_t)T, first + seg);
+  int* mine = hist + warp * BINS;
+  for (int pass = 0; pass < passes; ++pass) {
+    // which of the two buffers this pass writes: the last one writes `sorted`
+    int2* dst = (passes - 1 - pass) % 2 == 0 ? sorted : other;
+    const int2* src = dst == sorted ? other : sorted;
+    const int shift = pass * bits;
+    auto pair_at = [&](int64_t i) {
+      if (i >= last) return make_int2(-1, 0);
+      if (pass > 0) return __ldcg(src + i);
+      const int id = ids[i];
+      return make_int2(id >= 0 && id < V ? id : V, (int)i);
+    };
+    for (int b = threadIdx.x; b < SORT_WARPS * BINS; b += SORT_WARPS * 32) hist[b] = 0;
+    __syncthreads();
+    for (int64_t i = first; i < last; i += 32) {
+      const int2 p = pair_at(i + lane);
+      const int digit = p.x < 0 ? bins : (p.x >> shift) & (bins - 1);
+      const unsigned same = __match_any_sync(0xffffffffu, digit);
+      if (p.x >= 0 && lane == __ffs(same) - 1) mine[digit] += __popc(same);
+      __syncwarp();
+    }
+    __syncthreads();
+    int sum = 0;
+    if ((int)threadIdx.x < bins) {
+      for (int w = 0; w < SORT_WARPS; ++w) {
+        const int n = hist[w * BINS + threadIdx.x];
+        hist[w * BINS + threadIdx.x] = sum;
+        sum += n;
+      }
+      total[threadIdx.x] = sum;
+    }
+    whole_cluster_sync();
+    // exclusive sums over the bins of all CTAs, and the lower CTAs' pairs of the same bin
+    int all = 0, lower = 0;
+    if ((int)threadIdx.x < bins) {
+      for (int c = 0; c < ctas; ++c) {
+        const int n = ld_cluster_int(total + threadIdx.x, c);
+        all += n;
+        if (c < rank) lower += n;
+      }
+    }
+    int up = all;
+#pragma unroll
+    for (int s = 1; s < 32; s <<= 1) {
+      const int n = __shfl_up_sync(0xffffffffu, up, s);
+      if (lane >= s) up += n;
+    }
+    if (lane == 31) scan[warp] = up;
+    __syncthreads();
+    if (warp == 0) {
+      int n = scan[lane];
+#pragma unroll
+      for (int s = 1; s < 32; s <<= 1) {
+        const int m = __shfl_up_sync(0xffffffffu, n, s);
+        if (lane >= s) n += m;
+      }
+      scan[lane] = n;
+    }
+    __syncthreads();
+    if ((int)threadIdx.x < bins) base[threadIdx.x] = (warp > 0 ? scan[warp - 1] : 0) + up - all + lower;
+    __syncthreads();
+    for (int64_t i = first; i < last; i += 32) {
+      const int2 p = pair_at(i + lane);
+      const int digit = p.x < 0 ? bins : (p.x >> shift) & (bins - 1);
+      const unsigned same = __match_any_sync(0xffffffffu, digit);
+      int at = 0;
+      if (p.x >= 0) at = base[digit] + mine[digit];
+      __syncwarp();
+      if (p.x >= 0) {
+        dst[at + __popc(same & ((1u << lane) - 1))] = p;
+        if (lane == __ffs(same) - 1) mine[digit] += __popc(same);
+      }
+      __syncwarp();
+    }
+    __threadfence();
+    whole_cluster_sync();   // the pairs have arrived, and the counts have been read
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ sum
+struct SumArgs {
+  const void* dout;
+  const int* ids;
+  const int2* sorted;
+  void* dtable;
+  float* parts;    // [pieces][2][D]: of a run that comes from the piece before, of one that begins here and goes on
+  int T, D, V, piece, pieces, slabs, tpr;
+  float scale;
+  int accumulate;
+};
+
+constexpr int SUM_THREADS = 128;
+constexpr int FILL_WORDS = 4096;               // rows a CTA looks up at a time: a bit each
+
+template <class E, int V>
+__device__ __forceinline__ void put_row(E* at, const float (&acc)[V], float scale, int accumulate) {
+  float f[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) f[e] = acc[e] * scale;
+  Raw<E, V> r;
+  if (accumulate) {
+    float g[V];
+    r.load(at);
+    r.get(g);
+#pragma unroll
+    for (int e = 0; e < V; ++e) f[e] = fmaf(acc[e], scale, g[e]);
+  }
+  r.put(f);
+  r.store(at);
+}
+
+// E: table, O: tokens' rows.  A group of `tpr` threads takes a piece and a slab of tpr V columns.
+template <class E, class O, int V>
+__global__ void __launch_bounds__(SUM_THREADS) embed_sum_kernel(const SumArgs a) {
+  __shared__ uint32_t present[FILL_WORDS];
+  E* dtable = static_cast<E*>(a.dtable);
+  const int nvec = a.D / V;
+  if (!a.accumulate) {
+    const int64_t share = ((int64_t)a.V + gridDim.x - 1) / gridDim.x;
+    const int64_t begin = min((int64_t)a.V, blockIdx.x * share), end = min((int64_t)a.V, begin + share);
+    for (int64_t v0 = begin; v0 < end; v0 += FILL_WORDS * 32) {
+      const int n = (int)min((int64_t)FILL_WORDS * 32, end - v0);
+      for (int i = threadIdx.x; i < (n + 31) / 32; i += SUM_THREADS) present[i] = 0u;
+      __syncthreads();
+#pragma unroll 8
+      for (int t = threadIdx.x; t < a.T; t += SUM_THREADS) {
+        const int64_t at = (int64_t)a.ids[t] - v0;
+        if (at >= 0 && at < n) atomicOr(&present[at >> 5], 1u << (at & 31));
+      }
+      __syncthreads();
+      Raw<E, V> zero;
+      zero.clear();
+      for (int r = threadIdx.x >> 5; r < n; r += SUM_THREADS / 32) {
+        if ((present[r >> 5] >> (r & 31)) & 1u) continue;
+        E* row = dtable + (v0 + r) * a.D;
+        for (int c = threadIdx.x & 31; c < nvec; c += 32) zero.store(row + (int64_t)c * V);
+      }
+      __syncthreads();
+    }
+  }
+  wait_for_sort();
+  let_next_start();
+  const O* dout = static_cast<const O*>(a.dout);
+  const int groups = SUM_THREADS / a.tpr, lane = threadIdx.x % a.tpr;
+  const int64_t items = (int64_t)a.pieces * a.slabs;
+  for (int64_t item = (int64_t)blockIdx.x * groups + threadIdx.x / a.tpr; item < items; item += (int64_t)gridDim.x * groups) {
+    const int p = (int)(item / a.slabs), vec = (int)(item % a.slabs) * a.tpr + lane;
+    const int64_t first = (int64_t)p * a.piece, last = min((int64_t)a.T, first + a.piece);
+    const bool in = vec < nvec;
+    const int before = first > 0 ? __ldcg(a.sorted + first - 1).x : -1, after = last < a.T ? __ldcg(a.sorted + last).x : -1;
+    float acc[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) acc[e] = 0.f;
+    int run = -1;
+    // `run` ends: its row, or its part
+    auto flush = [&](bool goes_on) {
+      if (run < 0 || !in) return;
+      const bool came = run == before;
+      if (came || goes_on) {
+        float* at = a.parts + ((int64_t)p * 2 + (came ? 0 : 1)) * a.D + (int64_t)vec * V;
+#pragma unroll
+        for (int e = 0; e < V; ++e) at[e] = acc[e];
+      } else {
+        put_row<E, V>(dtable + (int64_t)run * a.D + (int64_t)vec * V, acc, a.scale, a.accumulate);
+      }
+    };
+    constexpr int U = 8;   // tokens in flight
+    for (int64_t i = first; i < last; i += U) {
+      int key[U];
+      Raw<O, V> r[U];
+      int2 pr[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) pr[u] = i + u < last ? __ldcg(a.sorted + i + u) : make_int2(a.V, 0);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        key[u] = pr[u].x < a.V ? pr[u].x : -1;   // padding stands last
+        r[u].clear();
+        if (key[u] >= 0 && in) r[u].load(dout + (int64_t)pr[u].y * a.D + (int64_t)vec * V);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (key[u] < 0) continue;
+        if (key[u] != run) {
+          flush(false);
+          run = key[u];
+#pragma unroll
+          for (int e = 0; e < V; ++e) acc[e] = 0.f;
+        }
+        float f[V];
+        r[u].get(f);
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[e] += f[e];
+      }
+    }
+    flush(run == after);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ join
+// Runs that cross pieces.  The piece in which such a run begins has it in its second part, the ones after it in their first.
+// A CTA takes 32 columns of the runs that begin in every gridDim.y-th piece; its warps add the parts in turn.
+constexpr int JOIN_WARPS = 8, JOIN_Y = 16;
+template <class E>
+__global__ void __launch_bounds__(JOIN_WARPS * 32) embed_join_kernel(const SumArgs a) {
+  __shared__ float sums[JOIN_WARPS][33];
+  __shared__ int begins[JOIN_WARPS * 32], count;
+  if (threadIdx.x == 0) count = 0;
+  wait_for_predecessor();
+  __syncthreads();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = blockIdx.x * 32 + lane;
+  E* dtable = static_cast<E*>(a.dtable);
+  auto key = [&](int64_t i) { return __ldcg(a.sorted + i).x; };
+  {   // all of this CTA's pieces at once: one that a run begins in and goes on from
+    const int p = blockIdx.y + threadIdx.x * gridDim.y;
+    if (p + 1 < a.pieces) {
+      const int64_t first = (int64_t)p * a.piece, end = first + a.piece;
+      const int run = key(end - 1), next = key(end), head = key(first), before = p > 0 ? key(first - 1) : -1;
+      if (run < a.V && next == run && !(head == run && before == run)) begins[atomicAdd(&count, 1)] = p;
+    }
+  }
+  __syncthreads();
+  for (int i = 0; i < count; ++i) {
+    const int p = begins[i], run = key((int64_t)(p + 1) * a.piece);
+    int lo = p + 1, hi = a.pieces;                                                // the last piece that begins with it lies in [lo, hi)
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (key((int64_t)mid * a.piece) == run) lo = mid; else hi = mid;
+    }
+    float s = 0.f;
+    if (c < a.D) {
+      if (warp == 0) s = a.parts[((int64_t)p * 2 + 1) * a.D + c];
+#pragma unroll 4
+      for (int q = p + 1 + warp; q <= lo; q += JOIN_WARPS) s += a.parts[(int64_t)q * 2 * a.D + c];
+    }
+    sums[warp][lane] = s;
+    __syncthreads();
+    if (warp == 0 && c < a.D) {
+#pragma unroll
+      for (int k = 1; k < JOIN_WARPS; ++k) s += sums[k][lane];
+      const float acc[1] = {s};
+      put_row<E, 1>(dtable + (int64_t)run * a.D + c, acc, a.scale, a.accumulate);
+    }
+    __syncthreads();
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ host
+int check(const bdlm_embed_params* p) {
+  if (p == nullptr || p->T < 0 || p->D <= 0 || p->V <= 0 || p->T > (1 << 30) || p->V > (1 << 30)) return BDLM_ERR_INVALID_ARG;
+  if (p->table_dtype < BDLM_BF16 || p->table_dtype > BDLM_FP32 || p->out_dtype < BDLM_BF16 || p->out_dtype > BDLM_FP32) return BDLM_ERR_INVALID_ARG;
+  if (p->out_dtype != p->table_dtype && p->table_dtype != BDLM_FP32) return BDLM_ERR_INVALID_ARG;
+  if (!isfinite(p->scale) || (p->accumulate != 0 && p->accumulate != 1) || p->reserved != 0) return BDLM_ERR_INVALID_ARG;
+  return BDLM_OK;
+}
+bool al(const void* x, unsigned bytes) { return (reinterpret_cast<uintptr_t>(x) & (bytes - 1)) == 0; }
+bool sm100() {
+  int dev = 0, major = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return false;
+  return cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) == cudaSuccess && major == 10;
+}
+size_t align256(size_t x) { return (x + 255) / 256 * 256; }
+
+constexpr int MAX_PIECES = 1024, MIN_PIECE = 8;
+static_assert(MAX_PIECES <= JOIN_Y * JOIN_WARPS * 32, "a thread of the join per piece");
+int piece_of(int T) { const int n = (T + MAX_PIECES - 1) / MAX_PIECES; return n < MIN_PIECE ? MIN_PIECE : n; }
+int pieces_of(int T) { return (T + piece_of(T) - 1) / piece_of(T); }
+size_t pairs_bytes(int T) { return align256((size_t)T * sizeof(int2)); }
+
+template <class T> struct Type { using type = T; };
+// Calls f(table type, row type).
+template <class F>
+void by_types(const bdlm_embed_params* p, F f) {
+  if (p->table_dtype == BDLM_BF16) f(Type<bf16_t>{}, Type<bf16_t>{});
+  else if (p->table_dtype == BDLM_FP16) f(Type<__half>{}, Type<__half>{});
+  else if (p->out_dtype == BDLM_BF16) f(Type<float>{}, Type<bf16_t>{});
+  else if (p->out_dtype == BDLM_FP16) f(Type<float>{}, Type<__half>{});
+  else f(Type<float>{}, Type<float>{});
+}
+int pow2_at_least(int n, int most) {
+  int p = 1;
+  while (p < n && p < most) p *= 2;
+  return p;
+}
+
+}  // namespace
+}  // namespace bdlm
+
+using namespace bdlm;
+
+extern "C" {
+
+size_t bdlm_embed_workspace_bytes(const bdlm_embed_params* p) {
+  if (check(p) != BDLM_OK) return 0;
+  return 2 * pairs_bytes(p->T) + align256((size_t)pieces_of(p->T) * 2 * p->D * sizeof(float));
+}
+
+int bdlm_embed_fwd(const bdlm_embed_params* p, const void* table, const int32_t* ids, void* out, void* cuda_stream) {
+  const int rc = check(p);
+  if (rc != BDLM_OK) return rc;
+  if (table == nullptr || (p->T > 0 && (ids == nullptr || out == nullptr))) return BDLM_ERR_INVALID_ARG;
+  if (!al(table, 16) || !al(out, 16) || !al(ids, 4)) return BDLM_ERR_INVALID_ARG;
+  if (!sm100()) return BDLM_ERR_UNSUPPORTED;
+  if (p->T == 0) return BDLM_OK;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const bool vec = p->D % 8 == 0;
+  const int nvec = vec ? p->D / 8 : p->D, tpr = pow2_at_least((nvec + 3) / 4, 256), rows = 256 / tpr;
+  const unsigned blocks = (unsigned)(((int64_t)p->T + rows - 1) / rows);
+  by_types(p, [&](auto e, auto o) {
+    using E = typename decltype(e)::type;
+    using O = typename decltype(o)::type;
+    auto kern = vec ? embed_fwd_kernel<E, O, 8> : embed_fwd_kernel<E, O, 1>;
+    kern<<<blocks, 256, 0, st>>>(static_cast<const E*>(table), ids, static_cast<O*>(out), p->T, p->D, p->V, tpr, p->scale);
+  });
+  return cudaGetLastError() == cudaSuccess ? BDLM_OK : BDLM_ERR_CUDA;
+}
+
+int bdlm_embed_bwd(const bdlm_embed_params* p, const void* dout, const int32_t* ids, void* dtable,
+                   void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  const int rc = check(p);
+  if (rc != BDLM_OK) return rc;
+  if (dtable == nullptr || (p->T > 0 && (dout == nullptr || ids == nullptr || workspace == nullptr))) return BDLM_ERR_INVALID_ARG;
+  if (!al(dout, 16) || !al(dtable, 16) || !al(workspace, 16) || !al(ids, 4)) return BDLM_ERR_INVALID_ARG;
+  if (workspace_bytes < bdlm_embed_workspace_bytes(p)) return BDLM_ERR_WORKSPACE_TOO_SMALL;
+  if (!sm100()) return BDLM_ERR_UNSUPPORTED;
+  if (p->T == 0 && p->accumulate) return BDLM_OK;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  char* ws = static_cast<char*>(workspace);
+  int2 *sorted = reinterpret_cast<int2*>(ws), *other = reinterpret_cast<int2*>(ws + pairs_bytes(p->T));
+  cudaError_t e = cudaSuccess;
+  if (p->T > 0) {
+    int key_bits = 1;
+    while ((1ll << key_bits) <= p->V) ++key_bits;   // keys 0 .. V
+    const int passes = (key_bits + DIGIT_BITS - 1) / DIGIT_BITS, bits = (key_bits + passes - 1) / passes;
+    const int ctas = p->T <= 2048 ? 1 : p->T <= 4096 ? 2 : p->T <= 8192 ? 4 : 8;
+    e = cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SORT_SMEM);
+    if (e == cudaSuccess)
+      e = launch_chained(embed_sort_kernel, false, ctas, SORT_WARPS * 32, SORT_SMEM, st, ctas, ids, p->T, p->V, passes, bits, sorted, other);
+    if (e != cudaSuccess) return BDLM_ERR_CUDA;
+  }
+  const bool vec = p->D % 8 == 0;
+  const int nvec = vec ? p->D / 8 : p->D;
+  SumArgs a = {};
+  a.dout = dout; a.ids = ids; a.sorted = sorted; a.dtable = dtable;
+  a.parts = reinterpret_cast<float*>(ws + 2 * pairs_bytes(p->T));
+  a.T = p->T; a.D = p->D; a.V = p->V; a.piece = piece_of(p->T); a.pieces = pieces_of(p->T);
+  a.tpr = pow2_at_least(nvec, SUM_THREADS); a.slabs = (nvec + a.tpr - 1) / a.tpr;
+  a.scale = p->scale; a.accumulate = p->accumulate;
+  const int64_t items = (int64_t)a.pieces * a.slabs, groups = SUM_THREADS / a.tpr;
+  int64_t want = (items + groups - 1) / groups;
+  if (!a.accumulate && want < ((int64_t)p->V + 15) / 16) want = ((int64_t)p->V + 15) / 16;
+  const int64_t cap = (int64_t)device_sm_count() * 8;
+  const unsigned blocks = (unsigned)(want < cap ? want : cap);
+  by_types(p, [&](auto te, auto to) {
+    using E = typename decltype(te)::type;
+    using O = typename decltype(to)::type;
+    e = vec ? launch_chained(embed_sum_kernel<E, O, 8>, p->T > 0, blocks, SUM_THREADS, 0, st, 1, a)
+            : launch_chained(embed_sum_kernel<E, O, 1>, p->T > 0, blocks, SUM_THREADS, 0, st, 1, a);
+    if (e != cudaSuccess || a.pieces < 2) return;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((p->D + 31) / 32), (unsigned)(a.pieces - 1 < JOIN_Y ? a.pieces - 1 : JOIN_Y));
+    cfg.blockDim = dim3(JOIN_WARPS * 32);
+    cfg.stream = st;
+    cudaLaunchAttribute attr = {};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, embed_join_kernel<E>, (const SumArgs)a);
+  });
+  return e == cudaSuccess ? BDLM_OK : BDLM_ERR_CUDA;
+}
+
+}  // extern "C"

@@ -1,0 +1,244 @@
+"""The token embedding against its fp64 oracle, through the binding.
+
+Tolerances.  The lookup is one fp32 product rounded once: (eps/2 + 2^-24) of the value.  A gradient row of n tokens is summed in
+fp32: at most `piece` additions in a piece (8, or T / 1024) and the pieces' parts in eight shares, so it is off by at most
+(piece + T / (8 piece) + 16) x 2^-24 of the sum of the terms' magnitudes, and rounded once."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import model_ops_oracle as orc
+from paper_2609_19242_b200 import binding
+
+pytestmark = pytest.mark.gpu
+
+BF16, FP16, FP32 = torch.bfloat16, torch.float16, torch.float32
+TYPES = [(BF16, BF16), (FP16, FP16), (FP32, FP32), (FP32, BF16), (FP32, FP16)]
+
+
+def _f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def _half_ulp(t):
+    return torch.finfo(t).eps / 2
+
+
+def _tiny(t):
+    """Half the distance of the type's smallest values."""
+    return torch.finfo(t).smallest_normal * torch.finfo(t).eps / 2
+
+
+def _ids(T, V, seed=0, masked=0.0, pad=0.05):
+    rng = np.random.default_rng(seed)
+    ids = np.minimum(((V + 1.0) ** rng.random(T)).astype(np.int64) - 1, V - 1)
+    ids[rng.random(T) < masked] = V - 1
+    ids[rng.random(T) < pad] = -1
+    return ids
+
+
+def _check_fwd(T, D, V, e=BF16, o=BF16, scale=1.0, ids=None):
+    g = torch.Generator().manual_seed(T + D)
+    table = torch.randn(V, D, generator=g).to(e).cuda()
+    ids = _ids(T, V, D) if ids is None else ids
+    out = binding.bdlm_embed_fwd(table, torch.tensor(ids, dtype=torch.int32, device="cuda"), scale=scale, dtype=o)
+    assert out.shape == (T, D) and out.dtype == o
+    ref = orc.embed_forward(_f64(table), ids, float(np.float32(scale)))
+    assert (np.abs(_f64(out) - ref) <= (_half_ulp(o) + 2.0 ** -24 + 2.0 ** -33) * np.abs(ref) + _tiny(o)).all()
+
+
+def _check_bwd(T, D, V, e=BF16, o=BF16, scale=1.0, ids=None, start=None, masked=0.0):
+    g = torch.Generator().manual_seed(T + D)
+    dout = torch.randn(T, D, generator=g).to(o).cuda()
+    ids = _ids(T, V, D, masked) if ids is None else np.asarray(ids)
+    dev = torch.tensor(ids, dtype=torch.int32, device="cuda")
+    if start is None:
+        out = torch.full((V, D), float("nan"), device="cuda", dtype=e)
+        binding.bdlm_embed_bwd(dout, dev, V, scale=scale, out=out)
+        again = binding.bdlm_embed_bwd(dout, dev, V, scale=scale, dtype=e)
+        assert torch.equal(out, again)   # bitwise reproducible
+        base = None
+    else:
+        first = torch.randn(V, D, generator=g).to(e).cuda()
+        out = first.clone()
+        binding.bdlm_embed_bwd(dout, dev, V, scale=scale, out=out, accumulate=True)
+        base = _f64(first)
+    s = float(np.float32(scale))
+    ref = orc.embed_backward(_f64(dout), ids, V, s, base)
+    size = orc.embed_backward(np.abs(_f64(dout)), ids, V, abs(s))
+    piece = max(8, -(-T // 1024))
+    off = (piece + T / (8 * piece) + 16) * 2.0 ** -24 * (size + (0 if base is None else np.abs(base)))
+    assert (np.abs(_f64(out) - ref) <= _half_ulp(e) * (np.abs(ref) + off) + off + _tiny(e)).all()
+    if base is not None:   # rows of tokens that do not occur stay as they were
+        absent = np.setdiff1d(np.arange(V), ids)
+        assert torch.equal(out[absent], first[absent])
+
+
+@pytest.mark.parametrize("D", [1, 3, 8, 24, 100, 128, 1001, 1024, 1544, 4096, 9000])
+@pytest.mark.parametrize("T", [1, 2, 7, 33, 500])
+def test_lookup_sizes(T, D):
+    _check_fwd(T, D, 300, scale=D ** 0.5)
+
+
+@pytest.mark.parametrize("e,o", TYPES)
+@pytest.mark.parametrize("D", [40, 77])
+def test_types(e, o, D):
+    _check_fwd(200, D, 50, e, o, scale=-0.7)
+    _check_bwd(200, D, 50, e, o, scale=-0.7)
+    _check_bwd(200, D, 50, e, o, scale=3.0, start=True)
+
+
+@pytest.mark.parametrize("T", [1, 2, 8, 9, 31, 64, 100, 1531, 2048, 2049, 4097, 8193, 20000])
+def test_gradient_numbers_of_tokens(T):
+    """Every cluster size of the sort, pieces of eight tokens and of more."""
+    _check_bwd(T, 40, 777, masked=0.3)
+
+
+@pytest.mark.parametrize("D", [1, 3, 8, 24, 100, 1001, 1024, 1032, 1544, 4096])
+def test_gradient_lengths_of_rows(D):
+    _check_bwd(300, D, 211, masked=0.25)
+    _check_bwd(300, D, 211, masked=0.25, start=True)
+
+
+@pytest.mark.parametrize("V", [1, 2, 511, 512, 513, 5000, 128256, 262144, 1 << 20])
+def test_gradient_sizes_of_the_table(V):
+    """One to four digits of the sort; tables far larger than the number of tokens."""
+    _check_bwd(600, 8, V, masked=0.2)
+
+
+@pytest.mark.parametrize("case", ["one", "alternating", "none", "beyond", "descending", "runs", "last_only", "mixed_pads"])
+@pytest.mark.parametrize("start", [None, True])
+def test_gradient_patterns_of_ids(case, start):
+    T, V = 3000, 97
+    t = np.arange(T)
+    ids = {"one": np.full(T, 41), "alternating": t % 2 * 96, "none": np.full(T, -1), "beyond": np.where(t % 3 == 0, V, np.where(t % 3 == 1, 2 ** 31 - 1, -2 ** 31)),
+           "descending": (T - 1 - t) % V, "runs": t // 40 % V, "last_only": np.where(t == T - 1, 5, -1), "mixed_pads": np.where(t % 2 == 0, -7, t % V)}[case]
+    _check_bwd(T, 72, V, FP32, FP32, ids=ids, start=start)
+
+
+def test_a_run_over_every_piece_and_its_neighbours():
+    """The mask token's run begins in one piece, covers many and ends in another, with short runs around it."""
+    T, V = 5000, 64
+    ids = np.concatenate([np.arange(13), np.full(4000, 30), np.arange(T - 4013) % 33 + 31])
+    rng = np.random.default_rng(3)
+    rng.shuffle(ids)
+    _check_bwd(T, 264, V, FP32, BF16, ids=ids, scale=0.125)
+    _check_bwd(T, 264, V, BF16, BF16, ids=ids, scale=0.125)
+
+
+def test_many_tokens():
+    _check_bwd(70001, 16, 3000, masked=0.5)
+
+
+def test_no_tokens():
+    table = torch.randn(10, 16, device="cuda").to(BF16)
+    ids = torch.empty(0, dtype=torch.int32, device="cuda")
+    assert binding.bdlm_embed_fwd(table, ids).shape == (0, 16)
+    dout = torch.empty(0, 16, device="cuda", dtype=BF16)
+    assert (binding.bdlm_embed_bwd(dout, ids, 10, out=table.clone()) == 0).all()
+    kept = table.clone()
+    binding.bdlm_embed_bwd(dout, ids, 10, out=kept, accumulate=True)
+    assert torch.equal(kept, table)
+
+
+def test_shapes_of_more_dimensions():
+    table = torch.randn(50, 24, device="cuda").to(BF16)
+    ids = torch.tensor(_ids(24, 50), dtype=torch.int32, device="cuda").view(2, 3, 4)
+    out = binding.bdlm_embed_fwd(table, ids, scale=2.0)
+    assert out.shape == (2, 3, 4, 24)
+    assert torch.equal(out.view(24, 24), binding.bdlm_embed_fwd(table, ids.view(-1), scale=2.0))
+    assert torch.equal(binding.bdlm_embed_bwd(out, ids, 50), binding.bdlm_embed_bwd(out.view(24, 24), ids.view(-1), 50))
+
+
+def test_ids_and_rows_of_any_alignment_within_the_rules():
+    """ids need four bytes only."""
+    table = torch.randn(50, 24, device="cuda").to(BF16)
+    ids = torch.tensor(_ids(41, 50), dtype=torch.int32, device="cuda")
+    assert torch.equal(binding.bdlm_embed_fwd(table, ids[1:]), binding.bdlm_embed_fwd(table, ids)[1:])
+    dout = torch.randn(40, 24, device="cuda").to(BF16)
+    assert torch.equal(binding.bdlm_embed_bwd(dout, ids[1:], 50), binding.bdlm_embed_bwd(dout, ids[1:].clone(), 50))
+
+
+def test_not_a_number_stays_with_its_token():
+    V, T = 40, 500
+    ids = _ids(T, V)
+    dout = torch.randn(T, 24, device="cuda").to(BF16)
+    dev = torch.tensor(ids, dtype=torch.int32, device="cuda")
+    want = binding.bdlm_embed_bwd(dout, dev, V)
+    bad = dout.clone()
+    bad[ids == 3] = float("nan")
+    bad[ids == -1] = float("inf")   # padding rows may hold anything
+    got = binding.bdlm_embed_bwd(bad, dev, V)
+    others = [v for v in range(V) if v != 3]
+    assert got[3].isnan().all() and torch.equal(got[others], want[others])
+
+
+def test_under_capture_on_another_stream_and_interleaved():
+    T, D, V = 3000, 264, 500
+    dout = torch.randn(T, D, device="cuda").to(BF16)
+    a = torch.tensor(_ids(T, V, 1, 0.4), dtype=torch.int32, device="cuda")
+    b = torch.tensor(_ids(T, V, 2, 0.1), dtype=torch.int32, device="cuda")
+    want = [binding.bdlm_embed_bwd(dout, i, V) for i in (a, b)]
+    # two streams at once, each with its own workspace
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(3):
+        for s, i in zip(streams, (a, b)):
+            with torch.cuda.stream(s):
+                got.append(binding.bdlm_embed_bwd(dout, i, V))
+    torch.cuda.synchronize()
+    for k, t in enumerate(got):
+        assert torch.equal(t, want[k % 2])
+    graph = torch.cuda.CUDAGraph()
+    ids = a.clone()
+    with torch.cuda.graph(graph):
+        rows = binding.bdlm_embed_fwd(want[0], ids)
+        grad = binding.bdlm_embed_bwd(dout, ids, V)
+    for i, w in zip((a, b, a), (want[0], want[1], want[0])):
+        ids.copy_(i)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(grad, w)
+        assert torch.equal(rows, binding.bdlm_embed_fwd(want[0], i))
+
+
+def test_gradient_of_a_tied_table_adds_to_the_loss_heads():
+    """The head's dW and the embedding's gradient in one buffer, as for a table that is both."""
+    T, D, V = 256, 128, 512
+    h, w = torch.randn(T, D, device="cuda").to(BF16), (0.05 * torch.randn(V, D, device="cuda")).to(BF16)
+    ids = torch.tensor(_ids(T, V, 5, 0.3), dtype=torch.int32, device="cuda")
+    labels = torch.tensor(_ids(T, V, 6), dtype=torch.int32, device="cuda")
+    _, _, lse = binding.bdlm_linear_ce_fwd(h, w, labels)
+    dh, dw = binding.bdlm_linear_ce_bwd(h, w, labels, lse)
+    got = dw.clone()
+    binding.bdlm_embed_bwd(dh, ids, V, scale=0.5, out=got, accumulate=True)
+    ref = orc.embed_backward(_f64(dh), ids.cpu().numpy(), V, 0.5, _f64(dw))
+    size = orc.embed_backward(np.abs(_f64(dh)), ids.cpu().numpy(), V, 0.5, np.abs(_f64(dw)))
+    off = 64 * 2.0 ** -24 * size
+    assert (np.abs(_f64(got) - ref) <= _half_ulp(BF16) * (np.abs(ref) + off) + off).all()
+
+
+def test_refusals():
+    table = torch.randn(10, 16, device="cuda").to(BF16)
+    ids = torch.zeros(4, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError):
+        binding.bdlm_embed_fwd(table, ids.long())
+    with pytest.raises(ValueError):
+        binding.bdlm_embed_fwd(table, ids.cpu())
+    with pytest.raises(binding.BdlmError):
+        binding.bdlm_embed_fwd(table, ids, dtype=FP32)
+    with pytest.raises(binding.BdlmError):
+        binding.bdlm_embed_fwd(table, ids, scale=float("inf"))
+    dout = torch.randn(4, 16, device="cuda").to(BF16)
+    with pytest.raises(ValueError):
+        binding.bdlm_embed_bwd(dout, ids[:3], 10)
+    with pytest.raises(ValueError):
+        binding.bdlm_embed_bwd(dout, ids, 10, accumulate=True)
+    with pytest.raises(ValueError):
+        binding.bdlm_embed_bwd(dout, ids, 10, out=torch.empty(11, 16, device="cuda", dtype=BF16))
+    with pytest.raises(binding.BdlmError) as e:
+        binding.bdlm_embed_bwd(dout, ids, 10, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+    assert e.value.status == -3
+    with pytest.raises(AssertionError):
+        binding.bdlm_embed_fwd(table[:, ::2], ids)
