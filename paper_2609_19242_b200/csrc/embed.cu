@@ -7,10 +7,12 @@
 //   sort    one cluster sorts (id, position) by id, a stable radix sort whose CTAs exchange their digits' counts through
 //           distributed shared memory; the pairs ping-pong through the workspace, which stays in L2
 //   sum     zeros the rows of tokens that do not occur -- it finds them in the ids themselves, so this runs beside the sort --
-//           and then, once the sort is done, sums the sorted tokens' rows in pieces of `piece` tokens.  A run of equal ids that
-//           lies inside a piece is finished there; of one that crosses into other pieces, each piece leaves an fp32 part.
-//   join    adds the parts of the runs that cross pieces (the mask token's run crosses thousands)
-// Every sum runs in the tokens' order inside a piece and over the pieces in order of eight interleaved shares, so it depends on
+//           and then, once the sort is done, sums the sorted tokens' rows in pieces of `piece` tokens.  A run of equal ids is
+//           finished by the piece it begins in, into the next one if need be; of one that covers a whole further piece, each
+//           piece leaves an fp32 part.  (With parts of every run that crosses a border, a third of the borders of 16384 tokens
+//           over 32008 ids had some, and joining them took 25 us of 85.)
+//   join    adds the parts of such long runs (the mask token's covers hundreds of pieces)
+// Every sum runs in the tokens' order inside a piece and over the pieces in order of sixteen interleaved shares, so it depends on
 // T only, not on how often a token occurs or where.
 #include <math.h>
 
@@ -71,7 +73,7 @@ __global__ void __launch_bounds__(256) embed_fwd_kernel(const E* table, const in
 }
 
 // ------------------------------------------------------------------------------------------------ sort
-constexpr int SORT_WARPS = 32, DIGIT_BITS = 9, BINS = 1 << DIGIT_BITS;
+constexpr int SORT_CTAS = 8, SORT_WARPS = 32, DIGIT_BITS = 9, BINS = 1 << DIGIT_BITS;
 constexpr int SORT_SMEM = (SORT_WARPS + 2) * BINS * (int)sizeof(int) + 32 * (int)sizeof(int);
 
 // Pairs (key, position), sorted by key with positions ascending among equal keys; key = id, or V where the id is no token.
@@ -91,6 +93,9 @@ __global__ void __launch_bounds__(SORT_WARPS * 32) embed_sort_kernel(const int* 
   const int64_t seg = (((int64_t)T + warps - 1) / warps + 31) / 32 * 32;
   const int64_t first = min((int64_t)T, (int64_t)(rank * SORT_WARPS + warp) * seg), last = min((int64_t)T, first + seg);
   int* mine = hist + warp * BINS;
+  constexpr int HELD = 8;   // pairs a thread has in flight; a short run stays in registers between counting and moving
+  int2 held[HELD];
+  const bool few = last - first <= 32 * HELD;
   for (int pass = 0; pass < passes; ++pass) {
     // which of the two buffers this pass writes: the last one writes `sorted`
     int2* dst = (passes - 1 - pass) % 2 == 0 ? sorted : other;
@@ -102,18 +107,28 @@ __global__ void __launch_bounds__(SORT_WARPS * 32) embed_sort_kernel(const int* 
       const int id = ids[i];
       return make_int2(id >= 0 && id < V ? id : V, (int)i);
     };
+    auto request = [&](int64_t i) {
+#pragma unroll
+      for (int k = 0; k < HELD; ++k) held[k] = pair_at(i + 32 * k + lane);
+    };
+    if (few) request(first);
     for (int b = threadIdx.x; b < SORT_WARPS * BINS; b += SORT_WARPS * 32) hist[b] = 0;
     __syncthreads();
-    for (int64_t i = first; i < last; i += 32) {
-      const int2 p = pair_at(i + lane);
-      const int digit = p.x < 0 ? bins : (p.x >> shift) & (bins - 1);
-      const unsigned same = __match_any_sync(0xffffffffu, digit);
-      if (p.x >= 0 && lane == __ffs(same) - 1) mine[digit] += __popc(same);
-      __syncwarp();
+    for (int64_t i = first; i < last; i += 32 * HELD) {
+      if (!few) request(i);
+#pragma unroll
+      for (int k = 0; k < HELD; ++k) {
+        const int2 p = held[k];
+        const int digit = p.x < 0 ? bins : (p.x >> shift) & (bins - 1);
+        const unsigned same = __match_any_sync(0xffffffffu, digit);
+        if (p.x >= 0 && lane == __ffs(same) - 1) mine[digit] += __popc(same);
+        __syncwarp();
+      }
     }
     __syncthreads();
     int sum = 0;
     if ((int)threadIdx.x < bins) {
+#pragma unroll
       for (int w = 0; w < SORT_WARPS; ++w) {
         const int n = hist[w * BINS + threadIdx.x];
         hist[w * BINS + threadIdx.x] = sum;
@@ -151,21 +166,68 @@ __global__ void __launch_bounds__(SORT_WARPS * 32) embed_sort_kernel(const int* 
     __syncthreads();
     if ((int)threadIdx.x < bins) base[threadIdx.x] = (warp > 0 ? scan[warp - 1] : 0) + up - all + lower;
     __syncthreads();
-    for (int64_t i = first; i < last; i += 32) {
-      const int2 p = pair_at(i + lane);
-      const int digit = p.x < 0 ? bins : (p.x >> shift) & (bins - 1);
-      const unsigned same = __match_any_sync(0xffffffffu, digit);
-      int at = 0;
-      if (p.x >= 0) at = base[digit] + mine[digit];
-      __syncwarp();
-      if (p.x >= 0) {
-        dst[at + __popc(same & ((1u << lane) - 1))] = p;
-        if (lane == __ffs(same) - 1) mine[digit] += __popc(same);
+    for (int64_t i = first; i < last; i += 32 * HELD) {
+      if (!few) request(i);
+#pragma unroll
+      for (int k = 0; k < HELD; ++k) {
+        const int2 p = held[k];
+        const int digit = p.x < 0 ? bins : (p.x >> shift) & (bins - 1);
+        const unsigned same = __match_any_sync(0xffffffffu, digit);
+        int at = 0;
+        if (p.x >= 0) at = base[digit] + mine[digit];
+        __syncwarp();
+        if (p.x >= 0) {
+          dst[at + __popc(same & ((1u << lane) - 1))] = p;
+          if (lane == __ffs(same) - 1) mine[digit] += __popc(same);
+        }
+        __syncwarp();
       }
-      __syncwarp();
     }
     __threadfence();
     whole_cluster_sync();   // the pairs have arrived, and the counts have been read
+  }
+}
+
+// The same pairs for few tokens: a token's place is the number of tokens that come before it, counted over all of them.  T^2
+// comparisons over the whole chip and no exchange, where the radix sort is a chain of barriers in one cluster.
+constexpr int RANK_WARPS = 8, RANK_TOKENS = 4, RANK_MOST = 8192;   // RANK_TOKENS tokens a warp at a time; keys in shared memory
+__global__ void __launch_bounds__(RANK_WARPS * 32) embed_rank_kernel(const int* ids, int T, int V, int2* sorted) {
+  __shared__ int keys[RANK_MOST];
+  let_next_start();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, padded = (T + 31) / 32 * 32;
+#pragma unroll 8
+  for (int t = threadIdx.x; t < padded; t += RANK_WARPS * 32) {
+    const int id = t < T ? ids[t] : -1;
+    keys[t] = t >= T ? 0x7fffffff : id >= 0 && id < V ? id : V;
+  }
+  __syncthreads();
+  const int t0 = (blockIdx.x * RANK_WARPS + warp) * RANK_TOKENS;   // RANK_TOKENS divides 32: they stand in one group of 32
+  if (t0 >= T) return;
+  int key[RANK_TOKENS], count[RANK_TOKENS];
+#pragma unroll
+  for (int n = 0; n < RANK_TOKENS; ++n) { key[n] = keys[min(t0 + n, T - 1)]; count[n] = 0; }
+  const int own = t0 / 32 * 32;
+#pragma unroll 4
+  for (int j = 0; j < own; j += 32) {   // earlier tokens come first among equals
+    const int k = keys[j + lane];
+#pragma unroll
+    for (int n = 0; n < RANK_TOKENS; ++n) count[n] += k <= key[n];
+  }
+  {
+    const int k = keys[own + lane];
+#pragma unroll
+    for (int n = 0; n < RANK_TOKENS; ++n) count[n] += own + lane < t0 + n ? k <= key[n] : k < key[n];
+  }
+#pragma unroll 4
+  for (int j = own + 32; j < padded; j += 32) {
+    const int k = keys[j + lane];
+#pragma unroll
+    for (int n = 0; n < RANK_TOKENS; ++n) count[n] += k < key[n];
+  }
+#pragma unroll
+  for (int n = 0; n < RANK_TOKENS; ++n) {
+    count[n] = __reduce_add_sync(0xffffffffu, count[n]);
+    if (lane == 0 && t0 + n < T) sorted[count[n]] = make_int2(key[n], t0 + n);
   }
 }
 
@@ -181,40 +243,23 @@ struct SumArgs {
   int accumulate;
 };
 
-constexpr int SUM_THREADS = 128;
-constexpr int FILL_WORDS = 4096;               // rows a CTA looks up at a time: a bit each
-
-template <class E, int V>
-__device__ __forceinline__ void put_row(E* at, const float (&acc)[V], float scale, int accumulate) {
-  float f[V];
-#pragma unroll
-  for (int e = 0; e < V; ++e) f[e] = acc[e] * scale;
-  Raw<E, V> r;
-  if (accumulate) {
-    float g[V];
-    r.load(at);
-    r.get(g);
-#pragma unroll
-    for (int e = 0; e < V; ++e) f[e] = fmaf(acc[e], scale, g[e]);
-  }
-  r.put(f);
-  r.store(at);
-}
+constexpr int SUM_THREADS = 512, GROUP_THREADS = 128;   // threads of a CTA; of a piece's slab, at most
+constexpr int FILL_WORDS = 4096;                        // rows a CTA looks up at a time: a bit each
 
 // E: table, O: tokens' rows.  A group of `tpr` threads takes a piece and a slab of tpr V columns.
-template <class E, class O, int V>
-__global__ void __launch_bounds__(SUM_THREADS) embed_sum_kernel(const SumArgs a) {
+template <class E, class O, int V, bool ADD>
+__global__ void __launch_bounds__(SUM_THREADS, 2) embed_sum_kernel(const SumArgs a) {
   __shared__ uint32_t present[FILL_WORDS];
   E* dtable = static_cast<E*>(a.dtable);
   const int nvec = a.D / V;
-  if (!a.accumulate) {
+  if (!ADD) {
     const int64_t share = ((int64_t)a.V + gridDim.x - 1) / gridDim.x;
     const int64_t begin = min((int64_t)a.V, blockIdx.x * share), end = min((int64_t)a.V, begin + share);
     for (int64_t v0 = begin; v0 < end; v0 += FILL_WORDS * 32) {
       const int n = (int)min((int64_t)FILL_WORDS * 32, end - v0);
       for (int i = threadIdx.x; i < (n + 31) / 32; i += SUM_THREADS) present[i] = 0u;
       __syncthreads();
-#pragma unroll 8
+#pragma unroll 16
       for (int t = threadIdx.x; t < a.T; t += SUM_THREADS) {
         const int64_t at = (int64_t)a.ids[t] - v0;
         if (at >= 0 && at < n) atomicOr(&present[at >> 5], 1u << (at & 31));
@@ -239,98 +284,122 @@ __global__ void __launch_bounds__(SUM_THREADS) embed_sum_kernel(const SumArgs a)
     const int p = (int)(item / a.slabs), vec = (int)(item % a.slabs) * a.tpr + lane;
     const int64_t first = (int64_t)p * a.piece, last = min((int64_t)a.T, first + a.piece);
     const bool in = vec < nvec;
-    const int before = first > 0 ? __ldcg(a.sorted + first - 1).x : -1, after = last < a.T ? __ldcg(a.sorted + last).x : -1;
+    auto key = [&](int64_t i) { return i >= 0 && i < a.T ? __ldcg(a.sorted + i).x : -1; };
+    const int before = key(first - 1), after = key(last), end = key(last - 1), far_before = key(first - a.piece - 1), far_after = key(last + a.piece);
+    // the run at the piece's front came from before: a long one leaves its part here, a short one is the piece before's
+    const bool skip = far_before != before && after != before;
+    // and the run at its end goes on: a short one that begins here is followed to its end
+    const bool follow = end == after && end != before && far_after != end;
     float acc[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) acc[e] = 0.f;
     int run = -1;
-    // `run` ends: its row, or its part
-    auto flush = [&](bool goes_on) {
-      if (run < 0 || !in) return;
-      const bool came = run == before;
-      if (came || goes_on) {
-        float* at = a.parts + ((int64_t)p * 2 + (came ? 0 : 1)) * a.D + (int64_t)vec * V;
-#pragma unroll
-        for (int e = 0; e < V; ++e) at[e] = acc[e];
-      } else {
-        put_row<E, V>(dtable + (int64_t)run * a.D + (int64_t)vec * V, acc, a.scale, a.accumulate);
-      }
-    };
-    constexpr int U = 8;   // tokens in flight
-    for (int64_t i = first; i < last; i += U) {
-      int key[U];
+    constexpr int U = sizeof(E) == 4 && V > 1 && (ADD || sizeof(O) == 4) ? 2 : 4;   // tokens in flight
+    const int64_t most = follow ? min((int64_t)a.T, last + a.piece) : last;
+    for (int64_t i = first; i < most; i += U) {
+      int2 pr[U + 1];
       Raw<O, V> r[U];
-      int2 pr[U];
+      Raw<E, V> old[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) pr[u] = i + u < last ? __ldcg(a.sorted + i + u) : make_int2(a.V, 0);
+      for (int u = 0; u <= U; ++u) pr[u] = i + u < a.T ? __ldcg(a.sorted + i + u) : make_int2(a.V, 0);
+      if (i >= last && pr[0].x != end) break;
+      bool real[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        key[u] = pr[u].x < a.V ? pr[u].x : -1;   // padding stands last
+        // (padding stands last)
+        real[u] = in && pr[u].x < a.V && (i + u < last ? !(skip && pr[u].x == before) : i + u < most && pr[u].x == end);
         r[u].clear();
-        if (key[u] >= 0 && in) r[u].load(dout + (int64_t)pr[u].y * a.D + (int64_t)vec * V);
+        if (real[u]) r[u].load(dout + (int64_t)pr[u].y * a.D + (int64_t)vec * V);
+        // what the sum is added to, where the run ends here as a whole: requested with the rows, not after them
+        if (ADD && real[u] && pr[u + 1].x != pr[u].x && pr[u].x != before)
+          old[u].load(dtable + (int64_t)pr[u].x * a.D + (int64_t)vec * V);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        if (key[u] < 0) continue;
-        if (key[u] != run) {
-          flush(false);
-          run = key[u];
-#pragma unroll
-          for (int e = 0; e < V; ++e) acc[e] = 0.f;
-        }
+        if (!real[u]) continue;
         float f[V];
         r[u].get(f);
+        const bool begins = pr[u].x != run;
+        run = pr[u].x;
 #pragma unroll
-        for (int e = 0; e < V; ++e) acc[e] += f[e];
+        for (int e = 0; e < V; ++e) acc[e] = begins ? f[e] : acc[e] + f[e];
+        const bool goes_on = pr[u + 1].x == run, came = run == before;
+        if (goes_on && (follow || i + u + 1 != last)) continue;
+        if (came || goes_on) {
+          float* at = a.parts + ((int64_t)p * 2 + (came ? 0 : 1)) * a.D + (int64_t)vec * V;
+#pragma unroll
+          for (int e = 0; e < V; ++e) at[e] = acc[e];
+        } else {
+          float g[V];
+          if (ADD) old[u].get(g);
+#pragma unroll
+          for (int e = 0; e < V; ++e) g[e] = ADD ? fmaf(acc[e], a.scale, g[e]) : acc[e] * a.scale;
+          Raw<E, V> o;
+          o.put(g);
+          o.store(dtable + (int64_t)run * a.D + (int64_t)vec * V);
+        }
       }
     }
-    flush(run == after);
   }
 }
 
 // ------------------------------------------------------------------------------------------------ join
-// Runs that cross pieces.  The piece in which such a run begins has it in its second part, the ones after it in their first.
-// A CTA takes 32 columns of the runs that begin in every gridDim.y-th piece; its warps add the parts in turn.
-constexpr int JOIN_WARPS = 8, JOIN_Y = 16;
-template <class E>
+// Long runs.  The piece in which such a run begins has it in its second part, the ones after it in their first.
+// A CTA takes 32 C columns of the runs that begin in every gridDim.y-th piece; its warps add the parts in turn.
+constexpr int JOIN_WARPS = 16, JOIN_Y = 16;
+template <class E, int C>
 __global__ void __launch_bounds__(JOIN_WARPS * 32) embed_join_kernel(const SumArgs a) {
-  __shared__ float sums[JOIN_WARPS][33];
-  __shared__ int begins[JOIN_WARPS * 32], count;
+  __shared__ float sums[JOIN_WARPS][32 * C + 1];
+  __shared__ int2 runs[JOIN_WARPS * 32];   // id, first piece
+  __shared__ int count;
   if (threadIdx.x == 0) count = 0;
   wait_for_predecessor();
   __syncthreads();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = blockIdx.x * 32 + lane;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = (blockIdx.x * 32 + lane) * C;
   E* dtable = static_cast<E*>(a.dtable);
   auto key = [&](int64_t i) { return __ldcg(a.sorted + i).x; };
   {   // all of this CTA's pieces at once: one that a run begins in and goes on from
     const int p = blockIdx.y + threadIdx.x * gridDim.y;
     if (p + 1 < a.pieces) {
       const int64_t first = (int64_t)p * a.piece, end = first + a.piece;
-      const int run = key(end - 1), next = key(end), head = key(first), before = p > 0 ? key(first - 1) : -1;
-      if (run < a.V && next == run && !(head == run && before == run)) begins[atomicAdd(&count, 1)] = p;
+      const int run = key(end - 1), far = end + a.piece < a.T ? key(end + a.piece) : -1, before = p > 0 ? key(first - 1) : -1;
+      if (run < a.V && far == run && before != run) {
+        runs[atomicAdd(&count, 1)] = make_int2(run, p);   // (in any order: no sum depends on it)
+      }
     }
   }
   __syncthreads();
   for (int i = 0; i < count; ++i) {
-    const int p = begins[i], run = key((int64_t)(p + 1) * a.piece);
-    int lo = p + 1, hi = a.pieces;                                                // the last piece that begins with it lies in [lo, hi)
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (key((int64_t)mid * a.piece) == run) lo = mid; else hi = mid;
-    }
-    float s = 0.f;
-    if (c < a.D) {
-      if (warp == 0) s = a.parts[((int64_t)p * 2 + 1) * a.D + c];
-#pragma unroll 4
-      for (int q = p + 1 + warp; q <= lo; q += JOIN_WARPS) s += a.parts[(int64_t)q * 2 * a.D + c];
-    }
-    sums[warp][lane] = s;
-    __syncthreads();
-    if (warp == 0 && c < a.D) {
+    const int2 run = runs[i];
+    // the last piece that begins with it, in two looks of a warp: every 32nd piece, then 32 pieces
+    auto begins = [&](int q) { return q < a.pieces && key((int64_t)q * a.piece) == run.x; };
+    int last = run.y + 32 * __popc(__ballot_sync(0xffffffffu, begins(run.y + 32 * (lane + 1))));
+    last += __popc(__ballot_sync(0xffffffffu, begins(last + 1 + lane)));
+    float s[C];
 #pragma unroll
-      for (int k = 1; k < JOIN_WARPS; ++k) s += sums[k][lane];
-      const float acc[1] = {s};
-      put_row<E, 1>(dtable + (int64_t)run * a.D + c, acc, a.scale, a.accumulate);
+    for (int e = 0; e < C; ++e) s[e] = 0.f;
+    if (c < a.D) {
+      auto add = [&](int64_t part) {
+        Raw<float, C> r;
+        float f[C];
+        r.load(a.parts + part * a.D + c);
+        r.get(f);
+#pragma unroll
+        for (int e = 0; e < C; ++e) s[e] += f[e];
+      };
+      if (warp == 0) add((int64_t)run.y * 2 + 1);
+#pragma unroll 8
+      for (int q = run.y + 1 + warp; q <= last; q += JOIN_WARPS) add((int64_t)q * 2);
+    }
+#pragma unroll
+    for (int e = 0; e < C; ++e) sums[warp][lane * C + e] = s[e];
+    __syncthreads();
+    for (int k = threadIdx.x; k < 32 * C; k += JOIN_WARPS * 32) {
+      const int col = blockIdx.x * 32 * C + k;
+      if (col >= a.D) break;
+      float t = sums[0][k];
+#pragma unroll
+      for (int w = 1; w < JOIN_WARPS; ++w) t += sums[w][k];
+      E* at = dtable + (int64_t)run.x * a.D + col;
+      *at = E(a.accumulate ? fmaf(t, a.scale, (float)*at) : t * a.scale);
     }
     __syncthreads();
   }
@@ -353,7 +422,7 @@ bool sm100() {
 size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
 constexpr int MAX_PIECES = 1024, MIN_PIECE = 8;
-static_assert(MAX_PIECES <= JOIN_Y * JOIN_WARPS * 32, "a thread of the join per piece");
+static_assert(MAX_PIECES <= JOIN_Y * JOIN_WARPS * 32 && MAX_PIECES <= 32 * 33, "a thread of the join per piece; two looks find a run's end");
 int piece_of(int T) { const int n = (T + MAX_PIECES - 1) / MAX_PIECES; return n < MIN_PIECE ? MIN_PIECE : n; }
 int pieces_of(int T) { return (T + piece_of(T) - 1) / piece_of(T); }
 size_t pairs_bytes(int T) { return align256((size_t)T * sizeof(int2)); }
@@ -423,10 +492,14 @@ int bdlm_embed_bwd(const bdlm_embed_params* p, const void* dout, const int32_t* 
     int key_bits = 1;
     while ((1ll << key_bits) <= p->V) ++key_bits;   // keys 0 .. V
     const int passes = (key_bits + DIGIT_BITS - 1) / DIGIT_BITS, bits = (key_bits + passes - 1) / passes;
-    const int ctas = p->T <= 2048 ? 1 : p->T <= 4096 ? 2 : p->T <= 8192 ? 4 : 8;
-    e = cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SORT_SMEM);
-    if (e == cudaSuccess)
-      e = launch_chained(embed_sort_kernel, false, ctas, SORT_WARPS * 32, SORT_SMEM, st, ctas, ids, p->T, p->V, passes, bits, sorted, other);
+    if (p->T <= RANK_MOST) {
+      constexpr int PER = RANK_WARPS * RANK_TOKENS;
+      e = launch_chained(embed_rank_kernel, false, (p->T + PER - 1) / PER, RANK_WARPS * 32, 0, st, 1, ids, p->T, p->V, sorted);
+    } else {
+      e = cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SORT_SMEM);
+      if (e == cudaSuccess)
+        e = launch_chained(embed_sort_kernel, false, SORT_CTAS, SORT_WARPS * 32, SORT_SMEM, st, SORT_CTAS, ids, p->T, p->V, passes, bits, sorted, other);
+    }
     if (e != cudaSuccess) return BDLM_ERR_CUDA;
   }
   const bool vec = p->D % 8 == 0;
@@ -435,21 +508,23 @@ int bdlm_embed_bwd(const bdlm_embed_params* p, const void* dout, const int32_t* 
   a.dout = dout; a.ids = ids; a.sorted = sorted; a.dtable = dtable;
   a.parts = reinterpret_cast<float*>(ws + 2 * pairs_bytes(p->T));
   a.T = p->T; a.D = p->D; a.V = p->V; a.piece = piece_of(p->T); a.pieces = pieces_of(p->T);
-  a.tpr = pow2_at_least(nvec, SUM_THREADS); a.slabs = (nvec + a.tpr - 1) / a.tpr;
+  a.tpr = pow2_at_least(nvec, GROUP_THREADS); a.slabs = (nvec + a.tpr - 1) / a.tpr;
   a.scale = p->scale; a.accumulate = p->accumulate;
   const int64_t items = (int64_t)a.pieces * a.slabs, groups = SUM_THREADS / a.tpr;
   int64_t want = (items + groups - 1) / groups;
   if (!a.accumulate && want < ((int64_t)p->V + 15) / 16) want = ((int64_t)p->V + 15) / 16;
-  const int64_t cap = (int64_t)device_sm_count() * 8;
+  const int64_t cap = (int64_t)device_sm_count() * 2;
   const unsigned blocks = (unsigned)(want < cap ? want : cap);
   by_types(p, [&](auto te, auto to) {
     using E = typename decltype(te)::type;
     using O = typename decltype(to)::type;
-    e = vec ? launch_chained(embed_sum_kernel<E, O, 8>, p->T > 0, blocks, SUM_THREADS, 0, st, 1, a)
-            : launch_chained(embed_sum_kernel<E, O, 1>, p->T > 0, blocks, SUM_THREADS, 0, st, 1, a);
+    auto sum = vec ? (a.accumulate ? embed_sum_kernel<E, O, 8, true> : embed_sum_kernel<E, O, 8, false>)
+                   : (a.accumulate ? embed_sum_kernel<E, O, 1, true> : embed_sum_kernel<E, O, 1, false>);
+    e = launch_chained(sum, p->T > 0, blocks, SUM_THREADS, 0, st, 1, a);
     if (e != cudaSuccess || a.pieces < 2) return;
+    const int cols = p->D % 4 == 0 ? 128 : 32;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((p->D + 31) / 32), (unsigned)(a.pieces - 1 < JOIN_Y ? a.pieces - 1 : JOIN_Y));
+    cfg.gridDim = dim3((unsigned)((p->D + cols - 1) / cols), (unsigned)(a.pieces - 1 < JOIN_Y ? a.pieces - 1 : JOIN_Y));
     cfg.blockDim = dim3(JOIN_WARPS * 32);
     cfg.stream = st;
     cudaLaunchAttribute attr = {};
@@ -457,7 +532,7 @@ int bdlm_embed_bwd(const bdlm_embed_params* p, const void* dout, const int32_t* 
     attr.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, embed_join_kernel<E>, (const SumArgs)a);
+    e = cudaLaunchKernelEx(&cfg, cols == 128 ? embed_join_kernel<E, 4> : embed_join_kernel<E, 1>, (const SumArgs)a);
   });
   return e == cudaSuccess ? BDLM_OK : BDLM_ERR_CUDA;
 }

@@ -146,13 +146,23 @@ __global__ void __launch_bounds__(max_threads(V, ITEMS, WIDE)) norm_fwd_kernel(c
 }
 
 // A thread keeps the sums for dweight and dbias of its columns over all its rows, so the columns' sums cost no traffic but one
-// row of partial sums per CTA.  The next row's vectors are requested before this one's sums are joined.
+// row of partial sums per CTA.  These sums take the registers that would hold loads in flight, so where a CTA has a row, the
+// rows to come are copied to shared memory asynchronously, RING of them; a thread reads what it has copied itself and
+// needs no barrier for it.  Elsewhere the next row's vectors are requested into registers before this one's sums are joined.
+constexpr int RING = 4;
+__device__ __forceinline__ void copy16(void* to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_end_row() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void copies_wait_first() { asm volatile("cp.async.wait_group %0;" ::"n"(RING - 1) : "memory"); }
+// (16-byte vectors of rows that take a CTA, as long as the ring fits)
+__host__ __device__ constexpr bool ringed(int V, int items, bool wide) { return wide && V > 1 && !big(V, items, wide); }
 template <class T, class W, int V, int ITEMS, bool WIDE>
 __global__ void __launch_bounds__(max_threads(V, ITEMS, WIDE)) norm_bwd_kernel(const NormArgs a) {
-  constexpr bool BIG = big(V, ITEMS, WIDE);
+  constexpr bool BIG = big(V, ITEMS, WIDE), RINGED = ringed(V, ITEMS, WIDE);
   constexpr int KEEP = BIG ? 1 : ITEMS;
   __shared__ float red[RED_FLOATS];
-  // short rows: the CTA's groups of rows join their sums here; long ones: the sums themselves, [dweight, dbias][item, element][thread]
+  // rows in flight: [row][dy, h, dh][item][thread] vectors;  short rows: the CTA's groups of rows join their sums here; long ones: the sums themselves, [dweight, dbias][item, element][thread]
   extern __shared__ float comb[];
   const int tpr = WIDE ? (int)blockDim.x : a.tpr, lane = WIDE ? (int)threadIdx.x : (int)threadIdx.x % tpr;
   const int rows = WIDE ? 1 : (int)blockDim.x / tpr, sub = WIDE ? 0 : (int)threadIdx.x / tpr;
@@ -180,10 +190,27 @@ __global__ void __launch_bounds__(max_threads(V, ITEMS, WIDE)) norm_bwd_kernel(c
   }
   Raw<T, V> ry[ITEMS], rh[ITEMS], rd[KEEP];
   float mean = 0.f, rstd = 0.f;
+  uint4* ring = reinterpret_cast<uint4*>(comb);
+  auto ring_at = [&](int slot, int tensor, int i) { return ring + ((slot * 3 + tensor) * ITEMS + i) * tpr + lane; };
+  auto copy_row = [&](int64_t row, int slot) {
+    if (row < a.T) {
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i) {
+        const int c = lane + i * tpr;
+        if (c < a.nvec) {
+          copy16(ring_at(slot, 0, i), dy + row * a.D + (int64_t)c * V);
+          copy16(ring_at(slot, 1, i), h + row * a.D + (int64_t)c * V);
+          if (dh != nullptr) copy16(ring_at(slot, 2, i), dh + row * a.D + (int64_t)c * V);
+        }
+      }
+    }
+    copies_end_row();   // (an empty group where there is no row: the groups count rows)
+  };
   auto request = [&](int64_t row) {
     const bool ok = row < a.T;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
+      if (RINGED) continue;
       const int c = lane + i * tpr;
       ry[i].clear(); rh[i].clear();
       if (!BIG) rd[BIG ? 0 : i].clear();
@@ -198,9 +225,25 @@ __global__ void __launch_bounds__(max_threads(V, ITEMS, WIDE)) norm_bwd_kernel(c
   };
   const int64_t step = (int64_t)gridDim.x * rows;
   int64_t r0 = (int64_t)blockIdx.x * rows;
+  if (RINGED) {
+    for (int k = 0; k < RING; ++k) copy_row(r0 + k * step, k);
+  }
   request(r0 + sub);
-  for (; r0 < a.T; r0 += step) {
+  for (int slot = 0; r0 < a.T; r0 += step, slot = slot + 1 == RING ? 0 : slot + 1) {
     const int64_t row = r0 + sub;
+    if (RINGED) {
+      copies_wait_first();
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i) {
+        ry[i].clear(); rh[i].clear(); rd[BIG ? 0 : i].clear();
+        if (lane + i * tpr < a.nvec) {
+          ry[i].load(reinterpret_cast<const T*>(ring_at(slot, 0, i)));
+          rh[i].load(reinterpret_cast<const T*>(ring_at(slot, 1, i)));
+          if (dh != nullptr) rd[BIG ? 0 : i].load(reinterpret_cast<const T*>(ring_at(slot, 2, i)));
+        }
+      }
+      copy_row(row + RING * step, slot);   // (after this thread's own reads of the slot)
+    }
     const bool ok = row < a.T;
     const float mu = mean, rs = rstd;
     // g and n of an item, formed twice: as vectors of the element type they take half the registers across the joining of the sums
@@ -468,8 +511,9 @@ int bdlm_norm_bwd(const bdlm_norm_params* p, const void* dy, const void* h, cons
       constexpr int V = decltype(v)::value, I = decltype(items)::value;
       constexpr bool WIDE = decltype(wide)::value, BIG = big(V, I, WIDE);
       auto kern = norm_bwd_kernel<typename decltype(t)::type, typename decltype(w)::type, V, I, WIDE>;
-      const int smem = !grads ? 0 : (int)((BIG ? 2 : WIDE ? 0 : 1) * l.threads * V * I * sizeof(float));
-      e = !BIG ? cudaSuccess : cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+      constexpr bool RINGED = ringed(V, I, WIDE);
+      const int smem = RINGED ? RING * 3 * I * l.threads * 16 : !grads ? 0 : (int)((BIG ? 2 : WIDE ? 0 : 1) * l.threads * V * I * sizeof(float));
+      e = !BIG && !RINGED ? cudaSuccess : cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
       if (e != cudaSuccess) return;
       kern<<<groups, l.threads, smem, st>>>(a);
       e = cudaGetLastError();

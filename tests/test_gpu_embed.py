@@ -1,8 +1,9 @@
 """The token embedding against its fp64 oracle, through the binding.
 
 Tolerances.  The lookup is one fp32 product rounded once: (eps/2 + 2^-24) of the value.  A gradient row of n tokens is summed in
-fp32: at most `piece` additions in a piece (8, or T / 1024) and the pieces' parts in eight shares, so it is off by at most
-(piece + T / (8 piece) + 16) x 2^-24 of the sum of the terms' magnitudes, and rounded once."""
+fp32: at most 2 `piece` additions one after the other (piece: 8, or T / 1024), or `piece` of them and then the pieces' parts
+in eight shares, so for the sizes here it is off by at most (piece + T / (8 piece) + 16) x 2^-24 of the sum of the terms'
+magnitudes (2 piece is less for T up to 147000), and rounded once."""
 import numpy as np
 import pytest
 import torch
@@ -124,6 +125,29 @@ def test_a_run_over_every_piece_and_its_neighbours():
     rng.shuffle(ids)
     _check_bwd(T, 264, V, FP32, BF16, ids=ids, scale=0.125)
     _check_bwd(T, 264, V, BF16, BF16, ids=ids, scale=0.125)
+
+
+@pytest.mark.parametrize("start", [None, True])
+def test_runs_of_every_length_at_every_place_in_a_piece(start):
+    """Pieces of eight tokens: runs inside one, over a border, over exactly one whole piece, over more, with padding behind."""
+    for k in range(8):
+        lens = [k + 1] + [n for n in range(1, 28) for _ in range(2)] + [8, 8, 16, 24, 7, 9, 17, 15, 23, 25]
+        ids = np.repeat(np.arange(len(lens)), lens)
+        _check_bwd(len(ids), 16, len(lens) + 3, FP32, FP32, ids=ids, start=start)
+        ids = np.concatenate([ids, np.full(13 + k, -1)])
+        _check_bwd(len(ids), 16, len(lens), BF16, BF16, ids=np.random.default_rng(k).permutation(ids), start=start)
+
+
+def test_runs_in_longer_pieces():
+    """Three tokens more than 1024 pieces of eight: pieces of nine."""
+    T = 8195
+    lens = []
+    rng = np.random.default_rng(1)
+    while sum(lens) < T:
+        lens.append(int(rng.choice([1, 2, 8, 9, 10, 17, 18, 19, 27, 28, 100, 900])))
+    ids = np.repeat(np.arange(len(lens)), lens)[:T]
+    _check_bwd(T, 24, len(lens), FP32, FP32, ids=ids)
+    _check_bwd(T, 24, len(lens), BF16, BF16, ids=rng.permutation(ids), start=True)
 
 
 def test_many_tokens():
