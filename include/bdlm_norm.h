@@ -37,10 +37,10 @@ extern "C" {
 #endif
 
 enum { BDLM_NORM_LAYER = 0, BDLM_NORM_RMS = 1 };
-enum { BDLM_NORM_MAX_D = 16384 };
+enum { BDLM_NORM_MAX_D = 32768 };
 
 typedef struct {
-  int32_t T, D;          /* T >= 0, 1 <= D <= BDLM_NORM_MAX_D (BDLM_ERR_UNSUPPORTED above) */
+  int32_t T, D;          /* 0 <= T <= 2^30, 1 <= D <= BDLM_NORM_MAX_D (BDLM_ERR_UNSUPPORTED above) */
   int32_t dtype;         /* BDLM_BF16, BDLM_FP16 or BDLM_FP32 */
   int32_t wdtype;        /* dtype or BDLM_FP32 */
   int32_t kind;          /* BDLM_NORM_LAYER or BDLM_NORM_RMS */
@@ -48,7 +48,7 @@ typedef struct {
   int32_t reserved[2];   /* 0 */
 } bdlm_norm_params;
 
-/* Scratch bytes of a backward that forms dweight (and dbias): fp32 partial sums of up to 592 groups of rows.  0 for invalid
+/* Scratch bytes of a backward that forms dweight (and dbias): fp32 partial sums of up to 148 groups of rows.  0 for invalid
  * parameters. */
 size_t bdlm_norm_workspace_bytes(const bdlm_norm_params* p);
 

@@ -28,7 +28,7 @@ EXPORTS = ("bdlm_workspace_bytes", "bdlm_attn_fwd", "bdlm_attn_bwd", "bdlm_lse_m
            "bdlm_norm_workspace_bytes", "bdlm_norm_fwd", "bdlm_norm_bwd", "bdlm_embed_workspace_bytes", "bdlm_embed_fwd",
            "bdlm_embed_bwd")
 LCE_WS_FWD, LCE_WS_BWD, LCE_WS_FWD_LEAST, LCE_WS_BWD_LEAST = 0, 1, 2, 3
-NORM_LAYER, NORM_RMS, NORM_MAX_D = 0, 1, 16384
+NORM_LAYER, NORM_RMS, NORM_MAX_D = 0, 1, 32768
 DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 STATIC_SCRATCH_ROWS = 1 << 20
 TRACE_SLOTS = 256

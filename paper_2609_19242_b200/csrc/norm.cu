@@ -1,17 +1,44 @@
 // Layer norm and root-mean-square norm of a residual stream, forward and backward (include/bdlm_norm.h).
 //
 // Both passes are streams over the [T, D] tensors, bound by memory: 4 T D elements each (x, residual, y, h; dy, h, dh, dx).  A row
-// is in registers from its load to its store, so each element is read and written once, and the variance is the sum of squares
-// around the mean that has been formed, not a difference of two large sums.  A row belongs to `tpr` threads: a whole CTA
-// where it has more than 128 vectors of 16 bytes, otherwise a warp or a power-of-two part of one, so that short rows fill the lanes.
-// Rows whose length is no multiple of a vector start anywhere and go element by element.
+// is read once and in registers until it is written, and the variance is the sum of squares around the mean that has been
+// formed, not a difference of two large sums.
+//
+// A row belongs to a part of a warp (a power of two of lanes) or a warp, to up to 32 warps, or, beyond 1024 threads, to a cluster
+// whose CTAs exchange their sums; a thread has two vectors of it.  An SM works on 1024 threads' worth of rows, so that the
+// chain of one row -- read, join the sums, write -- lies under the others'; 64 registers a thread are all there is for that, and the
+// backward's sums of two vectors of columns take half of them.  So nothing else of a row is kept: the rows to come are
+// copied to shared memory asynchronously, and a thread reads what it has copied itself, without a barrier, each time it
+// needs it.  (With the row's vectors in registers and half the threads, 16384 x 4096 bf16 took 101 us backward.)
+// A thread keeps its columns for all its rows, so the columns' sums cost a row of partial sums per CTA.
+//
+// Rows of a length that is no whole number of 16-byte vectors begin anywhere in a vector.  They are read as the vectors that cover
+// them, shifted by `shift` elements; a thread's rows are P apart, P the number of rows after which the shift repeats, so that
+// its columns stay its own.  (Element by element, 16384 x 4100 took 462 us forward and 1353 backward.)
 #include <math.h>
 
 #include "../../include/bdlm_norm.h"
 #include "elem_common.cuh"
+#include "tc_common.cuh"
 
 namespace bdlm {
 namespace {
+
+using tc::add_f32x2;
+using tc::fma_f32x2;
+using tc::mul_f32x2;
+using tc::pack_f32x2;
+using tc::unpack_f32x2;
+
+enum Span { NARROW, WIDE, TEAM };   // a row's threads: part of a warp or a warp; warps of a CTA; a cluster
+// Vectors of a row that a thread has.  Backward: 16 elements, or one vector of short rows.  Forward: up to four; with four and more
+// than a warp to a row, its weights are read again for each row instead of kept.
+__host__ __device__ constexpr int bwd_items(int V) { return 16 / V; }
+__host__ __device__ constexpr bool fwd_long(int items, Span s) { return s != NARROW && items == 4; }
+constexpr int NARROW_THREADS = 128, BWD_THREADS = 512;   // of a CTA, at most
+__host__ __device__ constexpr int fwd_threads(int V, int items, Span s) { return s == NARROW ? NARROW_THREADS : fwd_long(items, s) && V == 4 ? 1024 : 512; }
+// Rows in flight in the backward: the same number of bytes for 16- and 32-bit elements.
+__host__ __device__ constexpr int ring_of(int V) { return V == 8 ? 4 : 2; }
 
 struct NormArgs {
   const void *x, *res, *w, *b;     // forward; backward: dy, dh, weight
@@ -19,82 +46,216 @@ struct NormArgs {
   void *y, *h;                     // forward; backward: dx
   float *mean, *rstd;
   float* part;                     // backward: [dweight, dbias][groups][D], nullptr: neither is wanted
-  int T, D, nvec, tpr, rms;
+  int T, D, tpr, rms, period, team;
   float eps, inv_d;
 };
 
-constexpr int RED_FLOATS = 2 * 32 * 2;   // two buffers in turn, 32 warps, two sums
+// The rows and columns of a thread.  SHIFT: rows may begin inside a vector.
+template <int V, int ITEMS, Span S, bool SHIFT>
+struct Place {
+  int lane, sub, tpr, D;       // thread of the row's, which of the CTA's rows, and how many threads of it there are in this CTA
+  bool first;                  // the row's first thread
+  int64_t row, step;           // its first row, and how far apart they are
+  int col[ITEMS];              // of each vector's first element; negative where the vector begins before the row
+  bool has[ITEMS], whole[ITEMS];   // a vector there is; one that lies in the row altogether
+  __device__ __forceinline__ Place(const NormArgs& a) {
+    tpr = a.tpr;
+    sub = (int)threadIdx.x / tpr;
+    lane = (int)threadIdx.x - sub * tpr;
+    const int rows = (int)blockDim.x / tpr, period = SHIFT ? a.period : 1;
+    const int team = S == TEAM ? a.team : 1, rank = S == TEAM ? (int)tc::cluster_rank() : 0;
+    const int64_t seq = (int64_t)(blockIdx.x / team) * rows + sub;
+    row = seq;
+    step = (int64_t)gridDim.x / team * rows;   // a multiple of the period
+    D = a.D;
+    const int shift = SHIFT ? (int)((seq % period) * D % V) : 0;
+    const int all = (shift + D + V - 1) / V, share = (all + team - 1) / team;
+    const int begin = min(all, rank * share), vecs = min(share, all - begin);
+    first = lane == 0 && rank == 0;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      has[i] = lane + i * tpr < vecs;
+      col[i] = (begin + lane + i * tpr) * V - shift;
+      whole[i] = has[i] && (!SHIFT || (col[i] >= 0 && col[i] + V <= D));
+    }
+  }
+  __device__ __forceinline__ bool in(int i, int e) const { return has[i] && (unsigned)(col[i] + e) < (unsigned)D; }
+  // Elements of a vector that are not the row's become zeros.
+  template <class R>
+  __device__ __forceinline__ void trim(int i, R& r) const {
+    if (!SHIFT || whole[i]) return;
+    float f[V];
+    r.get(f);
+#pragma unroll
+    for (int e = 0; e < V; ++e) f[e] = in(i, e) ? f[e] : 0.f;
+    r.put(f);
+  }
+  template <class T, class R>
+  __device__ __forceinline__ void store(int i, T* row_of, const R& r) const {   // row_of: the row's first element
+    T* to = row_of + col[i];
+    if (whole[i]) r.store(to);
+    else if (SHIFT && has[i]) {
+      const T* e = reinterpret_cast<const T*>(&r);
+#pragma unroll
+      for (int k = 0; k < V; ++k) if (in(i, k)) to[k] = e[k];
+    }
+  }
+  // weight or bias of the thread's columns, zeros outside the row
+  template <class W>
+  __device__ __forceinline__ void columns(int i, const W* from, Raw<W, V>& r) const {
+    r.clear();
+    if (from == nullptr || !has[i]) return;
+    if (!SHIFT) { r.load(from + col[i]); return; }
+    W* e = reinterpret_cast<W*>(&r);
+#pragma unroll
+    for (int k = 0; k < V; ++k) if (in(i, k)) e[k] = from[col[i] + k];
+  }
+};
+__device__ __forceinline__ void copies_end_row() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int RING>
+__device__ __forceinline__ void copies_wait_first() { asm volatile("cp.async.wait_group %0;" ::"n"(RING - 1) : "memory"); }
+__device__ __forceinline__ void copies_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+// The vectors of the rows to come: [row][tensor][item][thread].
+template <class T, int TENSORS, int V, int ITEMS, Span S, bool SHIFT>
+struct Ring {
+  uint4* base;
+  const Place<V, ITEMS, S, SHIFT>& at;
+  int64_t elements;   // of the tensors
+  __device__ __forceinline__ uint4* slot(int k, int tensor, int i) const { return base + ((k * TENSORS + tensor) * ITEMS + i) * blockDim.x + threadIdx.x; }
+  __device__ __forceinline__ void copy(int k, int tensor, const T* from, int64_t row) const {
+    const int64_t start = row * at.D;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      if (!at.has[i]) continue;
+      const uint32_t to = (uint32_t)__cvta_generic_to_shared(slot(k, tensor, i));
+      if (SHIFT) {   // (the tensor may end inside its last vector)
+        const int bytes = (int)min((int64_t)V, elements - (start + at.col[i])) * (int)sizeof(T);
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from + start + at.col[i]), "r"(bytes) : "memory");
+      } else {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from + start + at.col[i]) : "memory");
+      }
+    }
+  }
+  // ok: there is such a row.  Elements of a vector that are not the row's become zeros.
+  __device__ __forceinline__ void read(int k, int tensor, int i, bool ok, Raw<T, V>& r) const {
+    r.clear();
+    if (ok && at.has[i]) r.load(reinterpret_cast<const T*>(slot(k, tensor, i)));
+    at.trim(i, r);
+  }
+};
 
-// Items a thread: few, so that weights, sums and the next row's vectors fit its registers beside the row's; for rows that would
-// need more than 512 threads of those, most_items of them, weights read again for each row and the backward's sums in shared memory.
-__host__ __device__ constexpr int mid_items(int V) { return V == 1 ? 4 : 2; }
-__host__ __device__ constexpr int most_items(int V) { return V == 1 ? 16 : 4; }
-__host__ __device__ constexpr bool big(int V, int items, bool wide) { return wide && items == most_items(V); }
-__host__ __device__ constexpr int max_threads(int V, int items, bool wide) { return !wide ? 128 : big(V, items, wide) && V < 8 ? 1024 : 512; }
-
-// Sums over the threads of a row; every thread gets them.  The order is fixed.
-template <bool WIDE, int N>
-__device__ __forceinline__ void row_sum(float (&v)[N], int tpr, float* red, int& turn) {
-  const int top = WIDE ? 16 : tpr / 2;
-  for (int s = top; s > 0; s >>= 1) {
+// Sums over the threads of a row; every thread gets them.  The order is fixed, and the same in all CTAs of a cluster.
+template <Span S, int N>
+__device__ __forceinline__ void row_sum(float (&v)[N], int tpr, int sub, int team, float* red, int& turn) {
+  for (int s = S == NARROW ? tpr / 2 : 16; s > 0; s >>= 1) {
 #pragma unroll
     for (int n = 0; n < N; ++n) v[n] += __shfl_xor_sync(0xffffffffu, v[n], s);
   }
-  if (!WIDE) return;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  if (S == NARROW) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = tpr >> 5;
   float* at = red + turn * 64;
   turn ^= 1;   // (a buffer is written again only after the barrier of the other one's use)
   if (lane == 0) {
 #pragma unroll
     for (int n = 0; n < N; ++n) at[warp * 2 + n] = v[n];
   }
-  __syncthreads();
+  if (S == TEAM) tc::cluster_sync();
+  else asm volatile("bar.sync %0, %1;" ::"r"(sub + 1), "r"(tpr) : "memory");   // the row's warps
+  at += sub * warps * 2;
 #pragma unroll
-  for (int n = 0; n < N; ++n) v[n] = lane < warps ? at[lane * 2 + n] : 0.f;
+  for (int n = 0; n < N; ++n) v[n] = S == WIDE && lane < warps ? at[lane * 2 + n] : 0.f;
+  if (S == TEAM && lane < warps) {
+    for (int c = 0; c < team; ++c) {   // (its own among them)
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        float u;
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(u) : "r"(tc::peer_addr(tc::smem_u32(at + lane * 2 + n), c)) : "memory");
+        v[n] += u;
+      }
+    }
+  }
 #pragma unroll
   for (int s = 16; s > 0; s >>= 1) {
 #pragma unroll
     for (int n = 0; n < N; ++n) v[n] += __shfl_xor_sync(0xffffffffu, v[n], s);
   }
 }
+constexpr int RED_FLOATS = 2 * 32 * 2;   // two buffers in turn, 32 warps, two sums
 
-template <class T, class W, int V, int ITEMS, bool WIDE>
-__global__ void __launch_bounds__(max_threads(V, ITEMS, WIDE)) norm_fwd_kernel(const NormArgs a) {
-  constexpr bool BIG = big(V, ITEMS, WIDE);
+// The forward loads a row's vectors straight into registers: a thread has nothing else to keep, so four CTAs of a 4096-element
+// row share an SM and their loads lie under one another.  (The backward's ring took 101 us here instead of 89, 16384 x 4096.)
+template <class T, class W, int V, int ITEMS, Span S, bool SHIFT>
+__global__ void __launch_bounds__(fwd_threads(V, ITEMS, S)) norm_fwd_kernel(const NormArgs a) {
+  constexpr bool LONG = fwd_long(ITEMS, S);
   __shared__ float red[RED_FLOATS];
-  const int tpr = WIDE ? (int)blockDim.x : a.tpr, lane = WIDE ? (int)threadIdx.x : (int)threadIdx.x % tpr;
-  const int rows = WIDE ? 1 : (int)blockDim.x / tpr, sub = WIDE ? 0 : (int)threadIdx.x / tpr;
+  const int tpr = S == NARROW ? a.tpr : (int)blockDim.x, lane = S == NARROW ? (int)threadIdx.x % tpr : (int)threadIdx.x;
+  const int rows = S == NARROW ? NARROW_THREADS / tpr : 1, sub = S == NARROW ? (int)threadIdx.x / tpr : 0;
+  const int team = S == TEAM ? a.team : 1;
+  const int seq = blockIdx.x / team * rows + sub, step = gridDim.x / team * rows;
+  const int shift = SHIFT ? (int)((int64_t)(seq % a.period) * a.D % V) : 0;
+  int begin = 0, vecs = (shift + a.D + V - 1) / V;
+  if (S == TEAM) {
+    const int share = (vecs + team - 1) / team;
+    begin = min(vecs, (int)tc::cluster_rank() * share);
+    vecs = min(vecs, begin + share);
+  }
+  const int first = begin + lane;
   int turn = 0;
+  // element e of vector c is column c V - shift + e; only a row's first and last vectors can be partly outside it
+  auto in = [&](int c, int e) { return c < vecs && (unsigned)(c * V - shift + e) < (unsigned)a.D; };
+  auto whole = [&](int c) { return c < vecs && (!SHIFT || (c * V >= shift && c * V - shift + V <= a.D)); };
+  auto load = [&](int c, const T* from, int row, Raw<T, V>& r) {
+    r.clear();
+    if (c >= vecs) return;
+    const int64_t at = (int64_t)row * a.D - shift + (int64_t)c * V;
+    if (!SHIFT || at + V <= (int64_t)a.T * a.D) r.load(from + at);   // (the tensor may end inside its last vector)
+    else {
+      T* e = reinterpret_cast<T*>(&r);
+#pragma unroll
+      for (int k = 0; k < V; ++k) if (in(c, k)) e[k] = from[at + k];
+    }
+  };
+  auto store = [&](int c, T* to, int row, const Raw<T, V>& r) {
+    const int64_t at = (int64_t)row * a.D - shift + (int64_t)c * V;
+    if (whole(c)) r.store(to + at);
+    else if (SHIFT) {
+      const T* e = reinterpret_cast<const T*>(&r);
+#pragma unroll
+      for (int k = 0; k < V; ++k) if (in(c, k)) to[at + k] = e[k];
+    }
+  };
+  auto columns = [&](int c, const void* p, Raw<W, V>& r) {
+    const W* from = static_cast<const W*>(p);
+    r.clear();
+    if (from == nullptr || c >= vecs) return;
+    if (!SHIFT) { r.load(from + (int64_t)c * V); return; }
+    W* e = reinterpret_cast<W*>(&r);
+#pragma unroll
+    for (int k = 0; k < V; ++k) if (in(c, k)) e[k] = from[c * V - shift + k];
+  };
   const T *x = static_cast<const T*>(a.x), *res = static_cast<const T*>(a.res);
   T *y = static_cast<T*>(a.y), *h = static_cast<T*>(a.h);
-  Raw<W, V> w[BIG ? 1 : ITEMS], b[BIG ? 1 : ITEMS];   // of this thread's columns, for all its rows
-  auto load_weight = [&](int i, int at) {
-    const int c = lane + i * tpr;
-    w[at].clear(); b[at].clear();
-    if (c < a.nvec && a.w != nullptr) w[at].load(static_cast<const W*>(a.w) + (int64_t)c * V);
-    if (c < a.nvec && a.b != nullptr) b[at].load(static_cast<const W*>(a.b) + (int64_t)c * V);
-  };
-  if (!BIG) {
+  Raw<W, V> w[LONG ? 1 : ITEMS], b[LONG ? 1 : ITEMS];   // of this thread's columns, for all its rows
+  if (!LONG) {
 #pragma unroll
-    for (int i = 0; i < (BIG ? 1 : ITEMS); ++i) load_weight(i, i);
+    for (int i = 0; i < (LONG ? 1 : ITEMS); ++i) { columns(first + i * tpr, a.w, w[i]); columns(first + i * tpr, a.b, b[i]); }
   }
-  for (int64_t r0 = (int64_t)blockIdx.x * rows; r0 < a.T; r0 += (int64_t)gridDim.x * rows) {
-    const int64_t row = r0 + sub;
+  for (int r0 = blockIdx.x / team * rows; r0 < a.T; r0 += step) {
+    const int row = r0 + sub;
     const bool ok = row < a.T;
     float f[ITEMS][V], s[1] = {0.f};
     Raw<T, V> rx[ITEMS], rr[ITEMS];
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-      const int c = lane + i * tpr;
       rx[i].clear(); rr[i].clear();
-      if (ok && c < a.nvec) {
-        rx[i].load(x + row * a.D + (int64_t)c * V);
-        if (res != nullptr) rr[i].load(res + row * a.D + (int64_t)c * V);
+      if (ok) {
+        load(first + i * tpr, x, row, rx[i]);
+        if (res != nullptr) load(first + i * tpr, res, row, rr[i]);
       }
     }
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-      const int c = lane + i * tpr;
+      const int c = first + i * tpr;
       rx[i].get(f[i]);
       if (res != nullptr) {   // the sum as it is stored is what is normalised
         float g[V];
@@ -103,235 +264,177 @@ __global__ void __launch_bounds__(max_threads(V, ITEMS, WIDE)) norm_fwd_kernel(c
         for (int e = 0; e < V; ++e) f[i][e] += g[e];
         rx[i].put(f[i]);
         rx[i].get(f[i]);
-        if (ok && c < a.nvec) rx[i].store(h + row * a.D + (int64_t)c * V);
+        if (ok) store(c, h, row, rx[i]);
+      }
+      if (SHIFT && !whole(c)) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) f[i][e] = in(c, e) ? f[i][e] : 0.f;
       }
 #pragma unroll
       for (int e = 0; e < V; ++e) s[0] += f[i][e];
     }
     float mean = 0.f;
     if (!a.rms) {
-      row_sum<WIDE>(s, tpr, red, turn);
+      row_sum<S>(s, tpr, 0, team, red, turn);
       mean = s[0] * a.inv_d;
     }
     s[0] = 0.f;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-      if (lane + i * tpr < a.nvec) {
+      const int c = first + i * tpr;
+      if (whole(c)) {
 #pragma unroll
         for (int e = 0; e < V; ++e) { const float t = f[i][e] - mean; s[0] = fmaf(t, t, s[0]); }
+      } else if (SHIFT) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) { const float t = in(c, e) ? f[i][e] - mean : 0.f; s[0] = fmaf(t, t, s[0]); }
       }
     }
-    row_sum<WIDE>(s, tpr, red, turn);
+    row_sum<S>(s, tpr, 0, team, red, turn);
     const float rstd = rsqrtf(fmaf(s[0], a.inv_d, a.eps));
-    if (ok && lane == 0) {
+    if (ok && first == 0) {
       if (a.mean != nullptr) a.mean[row] = mean;
       if (a.rstd != nullptr) a.rstd[row] = rstd;
     }
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-      const int c = lane + i * tpr;
+      const int c = first + i * tpr;
       float wf[V], bf[V];
-      if (BIG) load_weight(i, 0);
-      w[BIG ? 0 : i].get(wf);
-      b[BIG ? 0 : i].get(bf);
+      if (LONG) { columns(c, a.w, w[0]); columns(c, a.b, b[0]); }
+      w[LONG ? 0 : i].get(wf);
+      b[LONG ? 0 : i].get(bf);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         const float n = (f[i][e] - mean) * rstd;
         f[i][e] = a.w != nullptr ? fmaf(n, wf[e], bf[e]) : n;
       }
       rx[i].put(f[i]);
-      if (ok && c < a.nvec) rx[i].store(y + row * a.D + (int64_t)c * V);
+      if (ok) store(c, y, row, rx[i]);
     }
   }
+  if (S == TEAM) tc::cluster_sync();   // no CTA leaves while another one may still read its sums
 }
 
-// A thread keeps the sums for dweight and dbias of its columns over all its rows, so the columns' sums cost no traffic but one
-// row of partial sums per CTA.  These sums take the registers that would hold loads in flight, so where a CTA has a row, the
-// rows to come are copied to shared memory asynchronously, RING of them; a thread reads what it has copied itself and
-// needs no barrier for it.  Elsewhere the next row's vectors are requested into registers before this one's sums are joined.
-constexpr int RING = 4;
-__device__ __forceinline__ void copy16(void* to, const void* from) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
-}
-__device__ __forceinline__ void copies_end_row() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-__device__ __forceinline__ void copies_wait_first() { asm volatile("cp.async.wait_group %0;" ::"n"(RING - 1) : "memory"); }
-// (16-byte vectors of rows that take a CTA, as long as the ring fits)
-__host__ __device__ constexpr bool ringed(int V, int items, bool wide) { return wide && V > 1 && !big(V, items, wide); }
-template <class T, class W, int V, int ITEMS, bool WIDE>
-__global__ void __launch_bounds__(max_threads(V, ITEMS, WIDE)) norm_bwd_kernel(const NormArgs a) {
-  constexpr bool BIG = big(V, ITEMS, WIDE), RINGED = ringed(V, ITEMS, WIDE);
-  constexpr int KEEP = BIG ? 1 : ITEMS;
+// The products of a row's elements are packed two to an instruction: at 20 instructions an element, which they took one by one,
+// their issue was as long as the memory's time (16384 x 4096 bf16: MEASURED).
+template <class T, class W, int V, int ITEMS, Span S, bool SHIFT>
+__global__ void __launch_bounds__(BWD_THREADS) norm_bwd_kernel(const NormArgs a) {
+  constexpr int RING = ring_of(V);
   __shared__ float red[RED_FLOATS];
-  // rows in flight: [row][dy, h, dh][item][thread] vectors;  short rows: the CTA's groups of rows join their sums here; long ones: the sums themselves, [dweight, dbias][item, element][thread]
-  extern __shared__ float comb[];
-  const int tpr = WIDE ? (int)blockDim.x : a.tpr, lane = WIDE ? (int)threadIdx.x : (int)threadIdx.x % tpr;
-  const int rows = WIDE ? 1 : (int)blockDim.x / tpr, sub = WIDE ? 0 : (int)threadIdx.x / tpr;
-  int turn = 0;
+  extern __shared__ uint4 ring_mem[];
+  const Place<V, ITEMS, S, SHIFT> at(a);
+  const Ring<T, 3, V, ITEMS, S, SHIFT> ring{ring_mem, at, (int64_t)a.T * a.D};
   const T *dy = static_cast<const T*>(a.x), *h = static_cast<const T*>(a.h_in), *dh = static_cast<const T*>(a.res);
   T* dx = static_cast<T*>(a.y);
-  Raw<W, V> w[KEEP];
-  auto load_weight = [&](int i, int at) {
-    const int c = lane + i * tpr;
-    w[at].clear();
-    if (c < a.nvec && a.w != nullptr) w[at].load(static_cast<const W*>(a.w) + (int64_t)c * V);
-  };
-  float dw[KEEP][V], db[KEEP][V];
-#pragma unroll
-  for (int i = 0; i < ITEMS; ++i) {
-    if (!BIG) load_weight(i, BIG ? 0 : i);
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      if (!BIG) { dw[BIG ? 0 : i][e] = 0.f; db[BIG ? 0 : i][e] = 0.f; }
-      else if (a.part != nullptr) {
-        comb[(i * V + e) * tpr + lane] = 0.f;
-        comb[((ITEMS + i) * V + e) * tpr + lane] = 0.f;
-      }
-    }
-  }
-  Raw<T, V> ry[ITEMS], rh[ITEMS], rd[KEEP];
-  float mean = 0.f, rstd = 0.f;
-  uint4* ring = reinterpret_cast<uint4*>(comb);
-  auto ring_at = [&](int slot, int tensor, int i) { return ring + ((slot * 3 + tensor) * ITEMS + i) * tpr + lane; };
-  auto copy_row = [&](int64_t row, int slot) {
+  float next_mean = 0.f, next_rstd = 0.f;
+  auto copy_row = [&](int k, int64_t row) {
     if (row < a.T) {
-#pragma unroll
-      for (int i = 0; i < ITEMS; ++i) {
-        const int c = lane + i * tpr;
-        if (c < a.nvec) {
-          copy16(ring_at(slot, 0, i), dy + row * a.D + (int64_t)c * V);
-          copy16(ring_at(slot, 1, i), h + row * a.D + (int64_t)c * V);
-          if (dh != nullptr) copy16(ring_at(slot, 2, i), dh + row * a.D + (int64_t)c * V);
-        }
-      }
+      ring.copy(k, 0, dy, row);
+      ring.copy(k, 1, h, row);
+      if (dh != nullptr) ring.copy(k, 2, dh, row);
     }
     copies_end_row();   // (an empty group where there is no row: the groups count rows)
   };
-  auto request = [&](int64_t row) {
-    const bool ok = row < a.T;
-#pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-      if (RINGED) continue;
-      const int c = lane + i * tpr;
-      ry[i].clear(); rh[i].clear();
-      if (!BIG) rd[BIG ? 0 : i].clear();
-      if (ok && c < a.nvec) {
-        ry[i].load(dy + row * a.D + (int64_t)c * V);
-        rh[i].load(h + row * a.D + (int64_t)c * V);
-        if (!BIG && dh != nullptr) rd[BIG ? 0 : i].load(dh + row * a.D + (int64_t)c * V);
-      }
-    }
-    mean = ok && a.mean != nullptr ? a.mean[row] : 0.f;
-    rstd = ok ? a.rstd[row] : 0.f;
+  auto request_stats = [&](int64_t row) {
+    next_mean = row < a.T && !a.rms ? a.mean[row] : 0.f;
+    next_rstd = row < a.T ? a.rstd[row] : 0.f;
   };
-  const int64_t step = (int64_t)gridDim.x * rows;
-  int64_t r0 = (int64_t)blockIdx.x * rows;
-  if (RINGED) {
-    for (int k = 0; k < RING; ++k) copy_row(r0 + k * step, k);
-  }
-  request(r0 + sub);
-  for (int slot = 0; r0 < a.T; r0 += step, slot = slot + 1 == RING ? 0 : slot + 1) {
-    const int64_t row = r0 + sub;
-    if (RINGED) {
-      copies_wait_first();
+  for (int k = 0; k < RING; ++k) copy_row(k, at.row + k * at.step);
+  request_stats(at.row);
+  constexpr int H = V / 2;
+  Raw<W, V> weight[ITEMS];
+  uint64_t dw[ITEMS][H], db[ITEMS][H];   // pairs of columns
 #pragma unroll
-      for (int i = 0; i < ITEMS; ++i) {
-        ry[i].clear(); rh[i].clear(); rd[BIG ? 0 : i].clear();
-        if (lane + i * tpr < a.nvec) {
-          ry[i].load(reinterpret_cast<const T*>(ring_at(slot, 0, i)));
-          rh[i].load(reinterpret_cast<const T*>(ring_at(slot, 1, i)));
-          if (dh != nullptr) rd[BIG ? 0 : i].load(reinterpret_cast<const T*>(ring_at(slot, 2, i)));
-        }
-      }
-      copy_row(row + RING * step, slot);   // (after this thread's own reads of the slot)
-    }
+  for (int i = 0; i < ITEMS; ++i) {
+    at.columns(i, static_cast<const W*>(a.w), weight[i]);
+#pragma unroll
+    for (int e = 0; e < H; ++e) dw[i][e] = db[i][e] = 0ull;
+  }
+  int turn = 0, k = 0;
+  int64_t row = at.row;
+  for (int64_t done = 0; done < a.T; done += at.step, row += at.step, k = k + 1 == RING ? 0 : k + 1) {
     const bool ok = row < a.T;
-    const float mu = mean, rs = rstd;
-    // g and n of an item, formed twice: as vectors of the element type they take half the registers across the joining of the sums
-    Raw<T, V> cy[ITEMS], ch[ITEMS], cd[KEEP];
-    auto form = [&](int i, float (&y)[V], float (&g)[V], float (&n)[V]) {
-      float wf[V];
-      if (BIG) load_weight(i, 0);
-      cy[i].get(y);
-      ch[i].get(n);
-      w[BIG ? 0 : i].get(wf);
-      const bool in = lane + i * tpr < a.nvec;
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        n[e] = in ? (n[e] - mu) * rs : 0.f;
-        g[e] = a.w != nullptr ? y[e] * wf[e] : y[e];
-      }
-    };
-    float s[2] = {0.f, 0.f};
+    const float rs = next_rstd, minus = -next_mean * next_rstd;
+    const uint64_t rs2 = pack_f32x2(rs, rs), minus2 = pack_f32x2(minus, minus);
+    request_stats(row + at.step);
+    Raw<T, V> ry[ITEMS], rh[ITEMS];   // (as vectors of the element type they take half the registers across the joining of the sums)
+    uint64_t s0 = 0ull, s1 = 0ull;
+    copies_wait_first<RING>();
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-      float y[V], g[V], n[V];
-      cy[i] = ry[i]; ch[i] = rh[i];
-      if (!BIG) cd[BIG ? 0 : i] = rd[BIG ? 0 : i];
-      form(i, y, g, n);
+      float y[V], u[V], w[V];
+      ring.read(k, 0, i, ok, ry[i]);
+      ring.read(k, 1, i, ok, rh[i]);
+      weight[i].get(w);
+      ry[i].get(y);
+      rh[i].get(u);
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        s[0] = fmaf(g[e], n[e], s[0]);
-        s[1] += g[e];
-        if (!BIG) {
-          dw[BIG ? 0 : i][e] = fmaf(y[e], n[e], dw[BIG ? 0 : i][e]);
-          db[BIG ? 0 : i][e] += y[e];
-        } else if (a.part != nullptr) {
-          float *at = comb + (i * V + e) * tpr + lane, *at_b = at + ITEMS * V * tpr;
-          *at = fmaf(y[e], n[e], *at);
-          *at_b += y[e];
-        }
+      for (int e = 0; e < H; ++e) {
+        const uint64_t y2 = pack_f32x2(y[2 * e], y[2 * e + 1]), n2 = fma_f32x2(pack_f32x2(u[2 * e], u[2 * e + 1]), rs2, minus2);
+        const uint64_t g2 = a.w != nullptr ? mul_f32x2(y2, pack_f32x2(w[2 * e], w[2 * e + 1])) : y2;
+        s0 = fma_f32x2(g2, n2, s0);
+        s1 = add_f32x2(g2, s1);
+        dw[i][e] = fma_f32x2(y2, n2, dw[i][e]);
+        db[i][e] = add_f32x2(y2, db[i][e]);
       }
     }
-    if (!BIG) request(row + step);
-    row_sum<WIDE>(s, tpr, red, turn);
-    const float c2 = s[0] * a.inv_d, c1 = a.rms ? 0.f : s[1] * a.inv_d;
+    float s[2], p, q;
+    unpack_f32x2(s0, p, q);
+    s[0] = p + q;
+    unpack_f32x2(s1, p, q);
+    s[1] = p + q;
+    row_sum<S>(s, at.tpr, at.sub, a.team, red, turn);
+    const float c2 = -s[0] * a.inv_d * rs, c1 = a.rms ? 0.f : -s[1] * a.inv_d * rs;
+    const uint64_t c22 = pack_f32x2(c2, c2), c12 = pack_f32x2(c1, c1);
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-      const int c = lane + i * tpr;
-      float y[V], g[V], n[V], d[V];
-      form(i, y, g, n);
-      if (BIG) {
-        cd[0].clear();
-        if (dh != nullptr && c < a.nvec) cd[0].load(dh + row * a.D + (int64_t)c * V);
-      }
-      cd[BIG ? 0 : i].get(d);
+      float y[V], u[V], w[V], d[V];
+      Raw<T, V> rd, o;
+      rd.clear();
+      if (dh != nullptr) ring.read(k, 2, i, ok, rd);
+      rd.get(d);
+      weight[i].get(w);
+      ry[i].get(y);
+      rh[i].get(u);
 #pragma unroll
-      for (int e = 0; e < V; ++e) d[e] = fmaf(rs, g[e] - c1 - n[e] * c2, d[e]);
-      Raw<T, V> o;
+      for (int e = 0; e < H; ++e) {
+        const uint64_t n2 = fma_f32x2(pack_f32x2(u[2 * e], u[2 * e + 1]), rs2, minus2);
+        uint64_t g2 = pack_f32x2(y[2 * e], y[2 * e + 1]);
+        if (a.w != nullptr) g2 = mul_f32x2(g2, pack_f32x2(w[2 * e], w[2 * e + 1]));
+        const uint64_t t2 = add_f32x2(fma_f32x2(n2, c22, c12), pack_f32x2(d[2 * e], d[2 * e + 1]));
+        unpack_f32x2(fma_f32x2(g2, rs2, t2), d[2 * e], d[2 * e + 1]);
+      }
       o.put(d);
-      if (ok && c < a.nvec) o.store(dx + row * a.D + (int64_t)c * V);
+      if (ok) at.store(i, dx + row * a.D, o);
     }
-    if (BIG) request(row + step);
+    copy_row(k, row + RING * at.step);   // (after this thread's reads of the slot)
   }
+  copies_wait_all();
+  if (S == TEAM) tc::cluster_sync();   // no CTA leaves while the other one may still read its sums
   if (a.part == nullptr) return;
-  if (WIDE) {
+  float* comb = reinterpret_cast<float*>(ring_mem);   // the CTA's rows join their sums here
+  const int rows = blockDim.x / at.tpr, group = blockIdx.x / a.team, groups = gridDim.x / a.team;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    float* part = a.part + ((int64_t)which * groups + group) * a.D;
+    float* to = rows > 1 ? comb + (int64_t)at.sub * a.D : part;
+    __syncthreads();   // all rows' copies have landed, and the first sums have been read
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-      const int c = lane + i * tpr;
-      if (c < a.nvec) {
-        float* at = a.part + (int64_t)blockIdx.x * a.D + (int64_t)c * V;
-        float* at_b = at + (int64_t)gridDim.x * a.D;
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          at[e] = BIG ? comb[(i * V + e) * tpr + lane] : dw[BIG ? 0 : i][e];
-          at_b[e] = BIG ? comb[((ITEMS + i) * V + e) * tpr + lane] : db[BIG ? 0 : i][e];
-        }
+      for (int e = 0; e < H; ++e) {
+        float p, q;
+        unpack_f32x2(which ? db[i][e] : dw[i][e], p, q);
+        if (at.in(i, 2 * e)) to[at.col[i] + 2 * e] = p;
+        if (at.in(i, 2 * e + 1)) to[at.col[i] + 2 * e + 1] = q;
       }
     }
-  } else {
-    const int cols = tpr * ITEMS * V;   // of which D are there
-#pragma unroll
-    for (int which = 0; which < 2; ++which) {
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < ITEMS; ++i)
-#pragma unroll
-        for (int e = 0; e < V; ++e) comb[sub * cols + (lane + i * tpr) * V + e] = which ? db[BIG ? 0 : i][e] : dw[BIG ? 0 : i][e];
+    if (rows > 1) {
       __syncthreads();
       for (int c = threadIdx.x; c < a.D; c += blockDim.x) {
         float s = 0.f;
-        for (int r = 0; r < rows; ++r) s += comb[r * cols + c];
-        a.part[((int64_t)which * gridDim.x + blockIdx.x) * a.D + c] = s;
+        for (int r = 0; r < rows; ++r) s += comb[(int64_t)r * a.D + c];
+        part[c] = s;
       }
     }
   }
@@ -362,40 +465,70 @@ __global__ void __launch_bounds__(WG_WARPS * 32) norm_wgrad_kernel(const float* 
 }
 
 // ------------------------------------------------------------------------------------------------ host
-constexpr int MAX_GROUPS = 592;   // CTAs of a backward: four on each of 148 SMs
+constexpr int SMS = 148;   // what the launch shapes, and with them the workspace, count on: the device has them
 
-// How a row is laid over threads: V elements a vector, `items` vectors a thread.
-struct Layout { int vec, nvec, items, tpr, threads; bool wide; };
-Layout layout(const bdlm_norm_params* p) {
-  const int full = p->dtype == BDLM_FP32 ? 4 : 8;
-  Layout l;
-  l.vec = p->D % full == 0 ? full : 1;
-  l.nvec = p->D / l.vec;
-  const int most = most_items(l.vec), mid = mid_items(l.vec);
-  l.wide = l.nvec > 128;
-  if (!l.wide) {
-    l.tpr = 1;
-    while (l.tpr < 32 && l.tpr < l.nvec) l.tpr *= 2;
-    l.items = l.nvec <= 32 ? 1 : l.nvec <= 32 * mid ? mid : most;
-    l.threads = 128;
-  } else {
-    l.items = l.nvec <= 512 * mid ? mid : most;
-    l.threads = l.tpr = ((l.nvec + l.items - 1) / l.items + 31) / 32 * 32;
-  }
+// How the rows are laid over threads: `rows` of them in a CTA (a CTA's share of one in a team), tpr threads each.
+struct Layout { Span span; int vec, nvec, items, tpr, rows, period, team; };
+Layout vectors_of(const bdlm_norm_params* p) {
+  Layout l = {};
+  l.vec = p->dtype == BDLM_FP32 ? 4 : 8;
+  l.period = 1;
+  while ((int64_t)p->D * l.period % l.vec != 0) l.period *= 2;
+  l.nvec = l.period == 1 ? p->D / l.vec : (p->D + 2 * l.vec - 2) / l.vec;   // with the largest shift
   return l;
 }
-int64_t blocks_for_rows(const bdlm_norm_params* p, const Layout& l) {
-  const int rows = l.wide ? 1 : l.threads / l.tpr;
-  return ((int64_t)p->T + rows - 1) / rows;
+int up32(int n) { return (n + 31) / 32 * 32; }
+int narrow_tpr(int nvec, int items) {
+  int tpr = 1;
+  while (tpr * items < nvec) tpr *= 2;
+  return tpr;
 }
-int bwd_groups(const bdlm_norm_params* p, const Layout& l) {
-  const int per_sm = l.threads <= 128 ? 4 : l.threads <= 256 ? 2 : 1;
-  const int64_t want = blocks_for_rows(p, l), cap = MAX_GROUPS / 4 * per_sm;
-  return (int)(want < cap ? want : cap);
+Layout fwd_layout(const bdlm_norm_params* p) {
+  Layout l = vectors_of(p);
+  l.team = 1;
+  if (l.nvec <= 128) {
+    l.span = NARROW;
+    l.items = l.nvec <= 32 ? 1 : l.nvec <= 64 ? 2 : 4;
+    l.tpr = narrow_tpr(l.nvec, l.items);
+    l.rows = NARROW_THREADS / l.tpr;
+    return l;
+  }
+  l.items = l.nvec <= 2 * fwd_threads(l.vec, 2, WIDE) ? 2 : 4;
+  const int most = l.items * fwd_threads(l.vec, l.items, WIDE);
+  l.team = (l.nvec + most - 1) / most;
+  l.span = l.team > 1 ? TEAM : WIDE;
+  l.tpr = up32(((l.nvec + l.team - 1) / l.team + l.items - 1) / l.items);
+  l.rows = 1;
+  return l;
 }
+// The backward's CTAs have as many rows as fit, because those share partial sums, but none that leaves SMs without rows; whole
+// warps of NARROW ones, and a barrier of its own for each WIDE one, of 15 that there are.
+Layout bwd_layout(const bdlm_norm_params* p) {
+  Layout l = vectors_of(p);
+  l.items = l.nvec <= 32 ? 1 : bwd_items(l.vec);
+  l.team = (l.nvec + BWD_THREADS * l.items - 1) / (BWD_THREADS * l.items);
+  const int own = ((l.nvec + l.team - 1) / l.team + l.items - 1) / l.items;   // threads a CTA needs for a row
+  l.span = l.team > 1 ? TEAM : own > 32 ? WIDE : NARROW;
+  l.tpr = own > 32 ? up32(own) : narrow_tpr(own, 1);
+  const int64_t even = ((int64_t)p->T + SMS - 1) / SMS;
+  l.rows = l.span == TEAM ? 1 : BWD_THREADS / l.tpr;
+  if (l.span == WIDE && l.rows > 15) l.rows = 15;
+  if (l.rows > even) l.rows = even > 0 ? (int)even : 1;
+  if (l.span == NARROW) { const int per_warp = 32 / l.tpr; l.rows = (l.rows + per_warp - 1) / per_warp * per_warp; }
+  return l;
+}
+// CTAs, or clusters, of a launch: as many as have rows, at most `per_sm` an SM, and sequences of rows in whole periods.
+int groups_of(const bdlm_norm_params* p, const Layout& l, int per_sm) {
+  int unit = 1;
+  while (unit * l.rows % l.period != 0) unit *= 2;
+  const int64_t want = ((int64_t)p->T + l.rows - 1) / l.rows, cap = SMS * per_sm / l.team;
+  return (int)(want < cap ? (want + unit - 1) / unit * unit : cap / unit * unit);
+}
+int fwd_groups(const bdlm_norm_params* p, const Layout& l) { return groups_of(p, l, 2048 / (l.rows * l.tpr)); }
+int bwd_groups(const bdlm_norm_params* p, const Layout& l) { return groups_of(p, l, 1); }
 
 int check(const bdlm_norm_params* p) {
-  if (p == nullptr || p->T < 0 || p->D <= 0) return BDLM_ERR_INVALID_ARG;
+  if (p == nullptr || p->T < 0 || p->T > (1 << 30) || p->D <= 0) return BDLM_ERR_INVALID_ARG;
   if (p->dtype < BDLM_BF16 || p->dtype > BDLM_FP32 || (p->wdtype != p->dtype && p->wdtype != BDLM_FP32)) return BDLM_ERR_INVALID_ARG;
   if (p->kind != BDLM_NORM_LAYER && p->kind != BDLM_NORM_RMS) return BDLM_ERR_INVALID_ARG;
   if (!(p->eps >= 0.f) || isinf(p->eps) || p->reserved[0] != 0 || p->reserved[1] != 0) return BDLM_ERR_INVALID_ARG;
@@ -409,33 +542,31 @@ bool sm100() {
   return cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) == cudaSuccess && major == 10;
 }
 
-// Calls f(T, W, V, ITEMS, WIDE) with the call's types and layout as template arguments.
+// Calls f(T, W, V, SHIFT) with the call's types and vectors as template arguments.
 template <int N> using Int = std::integral_constant<int, N>;
 template <class T> struct Type { using type = T; };
 template <class F>
-void by_layout(const bdlm_norm_params* p, const Layout& l, F f) {
-  auto by_items = [&](auto t, auto w, auto v) {
-    constexpr int M = decltype(v)::value == 1 ? 4 : 2;
-    auto by_width = [&](auto items) {
-      if (l.wide) f(t, w, v, items, std::true_type{});
-      else f(t, w, v, items, std::false_type{});
-    };
-    if (l.items == 1) f(t, w, v, Int<1>{}, std::false_type{});
-    else if (l.items == M) by_width(Int<M>{});
-    else by_width(Int<4 * (M / 2) * (M / 2)>{});
-  };
-  auto by_vec = [&](auto t, auto w) {
-    constexpr int FULL = sizeof(typename decltype(t)::type) == 4 ? 4 : 8;
-    if (l.vec == 1) by_items(t, w, Int<1>{});
-    else by_items(t, w, Int<FULL>{});
+void by_types(const bdlm_norm_params* p, const Layout& l, F f) {
+  auto by_shift = [&](auto t, auto w) {
+    using V = Int<sizeof(typename decltype(t)::type) == 4 ? 4 : 8>;
+    if (l.period > 1) f(t, w, V{}, std::true_type{});
+    else f(t, w, V{}, std::false_type{});
   };
   auto by_weight = [&](auto t) {
-    if (p->wdtype == BDLM_FP32) by_vec(t, Type<float>{});
-    else by_vec(t, t);
+    if (p->wdtype == BDLM_FP32) by_shift(t, Type<float>{});
+    else by_shift(t, t);
   };
   if (p->dtype == BDLM_BF16) by_weight(Type<bf16_t>{});
   else if (p->dtype == BDLM_FP16) by_weight(Type<__half>{});
-  else by_vec(Type<float>{}, Type<float>{});
+  else by_shift(Type<float>{}, Type<float>{});
+}
+template <class K>
+cudaError_t launch_rows(K kern, const Layout& l, int groups, int smem, cudaStream_t st, const NormArgs& a) {
+  if (smem > 0) {
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+  }
+  return launch_chained(kern, false, (unsigned)(groups * l.team), l.rows * l.tpr, smem, st, l.team, a);
 }
 
 }  // namespace
@@ -447,7 +578,7 @@ extern "C" {
 
 size_t bdlm_norm_workspace_bytes(const bdlm_norm_params* p) {
   if (check(p) != BDLM_OK) return 0;
-  const size_t groups = (size_t)bwd_groups(p, layout(p));
+  const size_t groups = (size_t)bwd_groups(p, bwd_layout(p));
   return 2 * groups * p->D * sizeof(float);
 }
 
@@ -463,19 +594,25 @@ int bdlm_norm_fwd(const bdlm_norm_params* p, const void* x, const void* residual
   if (!al(mean, 4) || !al(rstd, 4)) return BDLM_ERR_INVALID_ARG;
   if (!sm100()) return BDLM_ERR_UNSUPPORTED;
   if (p->T == 0) return BDLM_OK;
-  const Layout l = layout(p);
+  const Layout l = fwd_layout(p);
   NormArgs a = {};
   a.x = x; a.res = residual; a.w = weight; a.b = bias; a.y = y; a.h = h; a.mean = mean; a.rstd = rstd;
-  a.T = p->T; a.D = p->D; a.nvec = l.nvec; a.tpr = l.tpr; a.rms = p->kind == BDLM_NORM_RMS; a.eps = p->eps;
+  a.T = p->T; a.D = p->D; a.tpr = l.tpr; a.rms = p->kind == BDLM_NORM_RMS; a.period = l.period; a.team = l.team; a.eps = p->eps;
   a.inv_d = (float)(1.0 / p->D);
-  const int64_t want = blocks_for_rows(p, l), cap = (int64_t)device_sm_count() * (2048 / l.threads);
-  const unsigned blocks = (unsigned)(want < cap ? want : cap);
-  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  by_layout(p, l, [&](auto t, auto w, auto v, auto items, auto wide) {
-    norm_fwd_kernel<typename decltype(t)::type, typename decltype(w)::type, decltype(v)::value, decltype(items)::value, decltype(wide)::value>
-        <<<blocks, l.threads, 0, st>>>(a);
+  cudaError_t e = cudaSuccess;
+  by_types(p, l, [&](auto t, auto w, auto v, auto shift) {
+    using X = typename decltype(t)::type;
+    using Wt = typename decltype(w)::type;
+    constexpr int V = decltype(v)::value;
+    constexpr bool SH = decltype(shift)::value;
+    void (*kern)(NormArgs) = l.span == TEAM  ? norm_fwd_kernel<X, Wt, V, 4, TEAM, SH>
+                             : l.span == WIDE ? (l.items == 2 ? norm_fwd_kernel<X, Wt, V, 2, WIDE, SH> : norm_fwd_kernel<X, Wt, V, 4, WIDE, SH>)
+                             : l.items == 1   ? norm_fwd_kernel<X, Wt, V, 1, NARROW, SH>
+                             : l.items == 2   ? norm_fwd_kernel<X, Wt, V, 2, NARROW, SH>
+                                              : norm_fwd_kernel<X, Wt, V, 4, NARROW, SH>;
+    e = launch_rows(kern, l, fwd_groups(p, l), 0, static_cast<cudaStream_t>(cuda_stream), a);
   });
-  return cudaGetLastError() == cudaSuccess ? BDLM_OK : BDLM_ERR_CUDA;
+  return e == cudaSuccess ? BDLM_OK : BDLM_ERR_CUDA;
 }
 
 int bdlm_norm_bwd(const bdlm_norm_params* p, const void* dy, const void* h, const void* weight, const float* mean,
@@ -496,27 +633,27 @@ int bdlm_norm_bwd(const bdlm_norm_params* p, const void* dy, const void* h, cons
   if (grads && p->T > 0 && workspace == nullptr) return BDLM_ERR_INVALID_ARG;
   if (grads && workspace_bytes < bdlm_norm_workspace_bytes(p)) return BDLM_ERR_WORKSPACE_TOO_SMALL;
   if (!sm100()) return BDLM_ERR_UNSUPPORTED;
-  const Layout l = layout(p);
+  const Layout l = bwd_layout(p);
   const int groups = bwd_groups(p, l);
   NormArgs a = {};
   a.x = dy; a.res = dh; a.w = weight; a.h_in = h; a.y = dx;
   a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);
   a.part = grads ? static_cast<float*>(workspace) : nullptr;
-  a.T = p->T; a.D = p->D; a.nvec = l.nvec; a.tpr = l.tpr; a.rms = p->kind == BDLM_NORM_RMS;
+  a.T = p->T; a.D = p->D; a.tpr = l.tpr; a.rms = p->kind == BDLM_NORM_RMS; a.period = l.period; a.team = l.team;
   a.inv_d = (float)(1.0 / p->D);
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   cudaError_t e = cudaSuccess;
   if (groups > 0) {
-    by_layout(p, l, [&](auto t, auto w, auto v, auto items, auto wide) {
-      constexpr int V = decltype(v)::value, I = decltype(items)::value;
-      constexpr bool WIDE = decltype(wide)::value, BIG = big(V, I, WIDE);
-      auto kern = norm_bwd_kernel<typename decltype(t)::type, typename decltype(w)::type, V, I, WIDE>;
-      constexpr bool RINGED = ringed(V, I, WIDE);
-      const int smem = RINGED ? RING * 3 * I * l.threads * 16 : !grads ? 0 : (int)((BIG ? 2 : WIDE ? 0 : 1) * l.threads * V * I * sizeof(float));
-      e = !BIG && !RINGED ? cudaSuccess : cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-      if (e != cudaSuccess) return;
-      kern<<<groups, l.threads, smem, st>>>(a);
-      e = cudaGetLastError();
+    by_types(p, l, [&](auto t, auto w, auto v, auto shift) {
+      using X = typename decltype(t)::type;
+      using Wt = typename decltype(w)::type;
+      constexpr int V = decltype(v)::value, I = bwd_items(V);
+      constexpr bool SH = decltype(shift)::value;
+      void (*kern)(NormArgs) = l.span == TEAM   ? norm_bwd_kernel<X, Wt, V, I, TEAM, SH>
+                               : l.span == WIDE ? norm_bwd_kernel<X, Wt, V, I, WIDE, SH>
+                               : l.items == 1   ? norm_bwd_kernel<X, Wt, V, 1, NARROW, SH>
+                                                : norm_bwd_kernel<X, Wt, V, I, NARROW, SH>;
+      e = launch_rows(kern, l, groups, ring_of(V) * 3 * l.items * l.rows * l.tpr * 16, st, a);
     });
     if (e != cudaSuccess) return BDLM_ERR_CUDA;
   }

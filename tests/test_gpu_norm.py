@@ -100,7 +100,7 @@ def _both(T, D, x=BF16, w=BF16, rms=False, affine=True, bias=True, residual=True
 
 # rows of part of a warp, of a warp, of a CTA; vectors and single elements; every items-per-thread variant and its borders
 @pytest.mark.parametrize("D", [1, 2, 7, 8, 24, 31, 64, 100, 127, 129, 256, 264, 512, 520, 1000, 1001, 1024, 1032, 1544, 2047, 2049, 4096,
-                               4104, 8192, 8200, 8191, 16383, 16384])
+                               4104, 8192, 8200, 8191, 16383, 16384, 16385, 20000, 32767, 32768])
 def test_lengths_of_rows(D):
     _both(5, D)
     _both(3, D, FP32, FP32, rms=True)
@@ -266,7 +266,7 @@ def test_refusals():
         binding.bdlm_norm_fwd(i["x"], None, i["b"])
     with pytest.raises(AssertionError):
         binding.bdlm_norm_fwd(i["x"][:, ::2], i["w"][::2].contiguous())
-    big = torch.zeros(1, 16392, device="cuda", dtype=BF16)
+    big = torch.zeros(1, 32776, device="cuda", dtype=BF16)
     with pytest.raises(binding.BdlmError) as e:
         binding.bdlm_norm_fwd(big)
     assert e.value.status == -2
