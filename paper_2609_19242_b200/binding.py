@@ -172,15 +172,30 @@ def _ptr(t):
 
 
 def _stream():
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    # (with tensors at hand CUDA is initialised; torch.cuda.current_device() would look that up again)
+    index = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else torch.cuda.current_device()
+    return torch._C._cuda_getCurrentRawStream(index)
 
 
-def _on_current_device(t):
-    """Launches go to the current device's stream: memory of another one would be out of the kernels' reach."""
-    if not t.is_cuda:
+def _current(t):
+    """Index of the current device, on which `t` has to be: launches go to its stream, and memory of another device would be out of
+    the kernels' reach."""
+    index = t.get_device()
+    if index < 0:
         raise ValueError("tensors must be CUDA tensors")
-    if t.device.index != torch.cuda.current_device():
+    if index != torch._C._cuda_getDevice():
         raise ValueError(f"the tensors are on {t.device}, which is not the current device")
+    return index
+
+
+def _checked(name, t, shape, dtype, index):
+    """Address of `t` (None: no such operand), which has to be contiguous, of this shape and type and on this device."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.shape != shape or t.get_device() != index:
+        raise ValueError(f"{name}: expected {dtype} {tuple(shape)} on cuda:{index}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    assert t.is_contiguous(), "tensors must be contiguous CUDA tensors"
+    return t.data_ptr()
 
 
 def _shape_params(q, k, block_size, **kw):
@@ -382,10 +397,10 @@ def bdlm_doc_table(cu_seqlens, L=None, device=None) -> DocTable:
 
 
 def _check_docs(docs, k_clean, kv_chunks):
-    _on_current_device(k_clean)
+    index = _current(k_clean)
     if docs.L != k_clean.shape[1]:
         raise ValueError("the table of documents is for another number of clean positions")
-    if docs.table.device != k_clean.device:
+    if docs.table.get_device() != index:
         raise ValueError("the table of documents is on another device")
     if kv_chunks is not None:
         raise ValueError("documents and gathered clean K/V (kv_chunks) cannot be combined")
@@ -567,43 +582,28 @@ def bdlm_norm_workspace_bytes(params: BdlmNormParams) -> int:
     return int(lib().bdlm_norm_workspace_bytes(ctypes.byref(params)))
 
 
-def _same(name, t, like, shape=None):
-    """`t` (if given) has the shape of `like` or `shape`, and lies on its device; the type too where no shape is given."""
-    if t is None:
-        return
-    if t.shape != (like.shape if shape is None else shape) or t.device != like.device or (shape is None and t.dtype != like.dtype):
-        raise ValueError(f"{name} does not match")
-
-
-def _row_stat(name, t, x):
-    _same(name, t, x, x.shape[:-1])
-    if t is not None and t.dtype != torch.float32:
-        raise ValueError(f"{name} must be fp32")
-
-
-def _check_weight(x, weight, **more):
-    for name, t in (("weight", weight), *more.items()):
-        _same(name, t, x, x.shape[-1:])
-        if t is not None and t.dtype != (x.dtype if weight is None else weight.dtype):
-            raise ValueError(f"{name} must be of the weight's type")
-
-
+# (A call on a few rows is bound by these functions, as the attention's are by theirs: every operand is looked at once.)
 def bdlm_norm_fwd(x, weight=None, bias=None, residual=None, *, eps=1e-5, rms=False, out=None):
     """Layer norm (root-mean-square norm with `rms`) of h = x + residual along the last axis: x [..., D] bf16, fp16 or fp32,
     weight and bias [D] of the same type or fp32.  Returns (y, h, mean, rstd): h is x itself where there is no residual, mean is None with
     `rms`; mean and rstd [...] fp32 are what the backward reads.  `out` may supply those four."""
-    _on_current_device(x)
-    D = x.shape[-1]
-    _same("residual", residual, x)
-    _check_weight(x, weight, bias=bias)
-    p = make_norm_params(x.numel() // D if D else 0, D, x.dtype, x.dtype if weight is None else weight.dtype, rms, eps)
+    index, shape, dtype = _current(x), x.shape, x.dtype
+    D, rows = shape[-1], shape[:-1]
+    wdtype = dtype if weight is None else weight.dtype
+    w_at, b_at = _checked("weight", weight, shape[-1:], wdtype, index), _checked("bias", bias, shape[-1:], wdtype, index)
+    res_at = _checked("residual", residual, shape, dtype, index)
     if out is None:
-        stat = lambda: torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-        out = (torch.empty_like(x), x if residual is None else torch.empty_like(x), None if rms else stat(), stat())
-    y, h, mean, rstd = out
-    _same("y", y, x), _same("h", h, x), _row_stat("mean", mean, x), _row_stat("rstd", rstd, x)
-    rc = lib().bdlm_norm_fwd(ctypes.byref(p), _ptr(x), _ptr(residual), _ptr(weight), _ptr(bias), _ptr(y),
-                             None if residual is None else _ptr(h), _ptr(mean), _ptr(rstd), _stream())
+        y, rstd = torch.empty_like(x), x.new_empty(rows, dtype=torch.float32)
+        h, mean = x if residual is None else torch.empty_like(x), None if rms else torch.empty_like(rstd)
+        out = (y, h, mean, rstd)
+        y_at, h_at, mean_at, rstd_at = y.data_ptr(), h.data_ptr(), None if rms else mean.data_ptr(), rstd.data_ptr()
+    else:
+        y, h, mean, rstd = out
+        y_at, h_at = _checked("y", y, shape, dtype, index), _checked("h", h, shape, dtype, index)
+        mean_at, rstd_at = _checked("mean", mean, rows, torch.float32, index), _checked("rstd", rstd, rows, torch.float32, index)
+    p = BdlmNormParams(x.numel() // D if D else 0, D, DTYPES[dtype], DTYPES[wdtype], NORM_RMS if rms else NORM_LAYER, eps)
+    rc = lib().bdlm_norm_fwd(ctypes.byref(p), _checked("x", x, shape, dtype, index), res_at, w_at, b_at, y_at,
+                             None if residual is None else h_at, mean_at, rstd_at, torch._C._cuda_getCurrentRawStream(index))
     if rc != 0:
         raise BdlmError(rc, "bdlm_norm_fwd")
     return out
@@ -613,20 +613,27 @@ def bdlm_norm_bwd(dy, h, weight, mean, rstd, *, dh=None, bias=False, rms=False, 
     """Backward: dy the gradient of y, dh (optional) the gradient that reaches h along the residual path; h, mean and rstd as the
     forward returned them.  Returns (dx, dweight, dbias): dx is the gradient of x and of the residual, dweight is None without a
     weight, dbias unless `bias`."""
-    _on_current_device(h)
-    D = h.shape[-1]
-    _same("dy", dy, h), _same("dh", dh, h), _row_stat("mean", mean, h), _row_stat("rstd", rstd, h)
-    _check_weight(h, weight)
-    p = make_norm_params(h.numel() // D if D else 0, D, h.dtype, h.dtype if weight is None else weight.dtype, rms)
+    index, shape, dtype = _current(h), h.shape, h.dtype
+    D, rows = shape[-1], shape[:-1]
+    wdtype = dtype if weight is None else weight.dtype
+    w_at = _checked("weight", weight, shape[-1:], wdtype, index)
     if out is None:
-        out = (torch.empty_like(h), None if weight is None else torch.empty_like(weight),
-               torch.empty_like(weight) if bias and weight is not None else None)
-    dx, dw, db = out
-    _same("dx", dx, h), _check_weight(h, weight, dweight=dw, dbias=db)
+        dx, dw = torch.empty_like(h), None if weight is None else torch.empty_like(weight)
+        db = torch.empty_like(weight) if bias and weight is not None else None
+        out = (dx, dw, db)
+        dx_at, dw_at, db_at = dx.data_ptr(), None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr()
+    else:
+        dx, dw, db = out
+        dx_at = _checked("dx", dx, shape, dtype, index)
+        dw_at, db_at = _checked("dweight", dw, shape[-1:], wdtype, index), _checked("dbias", db, shape[-1:], wdtype, index)
+    p = BdlmNormParams(h.numel() // D if D else 0, D, DTYPES[dtype], DTYPES[wdtype], NORM_RMS if rms else NORM_LAYER)
+    at = ctypes.byref(p)
     if workspace is None and (dw is not None or db is not None):
-        workspace = torch.empty(max(bdlm_norm_workspace_bytes(p), 16), dtype=torch.uint8, device=h.device)
-    rc = lib().bdlm_norm_bwd(ctypes.byref(p), _ptr(dy), _ptr(h), _ptr(weight), _ptr(mean), _ptr(rstd), _ptr(dh), _ptr(dx),
-                             _ptr(dw), _ptr(db), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream())
+        workspace = h.new_empty(max(lib().bdlm_norm_workspace_bytes(at), 16), dtype=torch.uint8)
+    rc = lib().bdlm_norm_bwd(at, _checked("dy", dy, shape, dtype, index), _checked("h", h, shape, dtype, index), w_at,
+                             _checked("mean", mean, rows, torch.float32, index), _checked("rstd", rstd, rows, torch.float32, index),
+                             _checked("dh", dh, shape, dtype, index), dx_at, dw_at, db_at, _ptr(workspace),
+                             0 if workspace is None else workspace.numel(), torch._C._cuda_getCurrentRawStream(index))
     if rc != 0:
         raise BdlmError(rc, "bdlm_norm_bwd")
     return out
@@ -646,15 +653,14 @@ def bdlm_embed_workspace_bytes(params: BdlmEmbedParams) -> int:
 def bdlm_embed_fwd(table, ids, *, scale=1.0, dtype=None, out=None):
     """Rows of table [V, D] for ids [...] int32 (outside [0, V): padding, a row of zeros), times `scale`.  Returns [..., D] of
     `dtype`: the table's (default), or any of bf16, fp16 and fp32 for an fp32 table."""
-    _on_current_device(table)
-    V, D = table.shape
-    if ids.dtype != torch.int32 or ids.device != table.device:
-        raise ValueError("ids must be int32, on the table's device")
+    index, (V, D) = _current(table), table.shape
+    ids_at = _checked("ids", ids, ids.shape, torch.int32, index)
+    shape = (*ids.shape, D)
     if out is None:
-        out = torch.empty(*ids.shape, D, dtype=table.dtype if dtype is None else dtype, device=table.device)
-    _same("out", out, table, (*ids.shape, D))
-    p = make_embed_params(ids.numel(), D, V, table.dtype, out.dtype, scale)
-    rc = lib().bdlm_embed_fwd(ctypes.byref(p), _ptr(table), _ptr(ids), _ptr(out), _stream())
+        out = table.new_empty(shape, dtype=table.dtype if dtype is None else dtype)
+    p = BdlmEmbedParams(ids.numel(), D, V, DTYPES[table.dtype], DTYPES[out.dtype], scale, 0)
+    rc = lib().bdlm_embed_fwd(ctypes.byref(p), _ptr(table), ids_at, _checked("out", out, shape, out.dtype, index),
+                              torch._C._cuda_getCurrentRawStream(index))
     if rc != 0:
         raise BdlmError(rc, "bdlm_embed_fwd")
     return out
@@ -663,19 +669,19 @@ def bdlm_embed_fwd(table, ids, *, scale=1.0, dtype=None, out=None):
 def bdlm_embed_bwd(dout, ids, V, *, scale=1.0, dtype=None, accumulate=False, out=None, workspace=None):
     """Gradient of the table [V, D] for dout [..., D], the gradient of bdlm_embed_fwd's result: of `dtype` (default: dout's;
     fp32 goes with any).  With `accumulate` it is added to `out`."""
-    _on_current_device(dout)
-    D = dout.shape[-1]
-    if ids.dtype != torch.int32 or ids.device != dout.device or dout.shape[:-1] != ids.shape:
-        raise ValueError("ids must be int32, one per row of dout, on its device")
+    index, shape = _current(dout), dout.shape
+    D = shape[-1]
+    ids_at = _checked("ids", ids, shape[:-1], torch.int32, index)
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs the gradient to add to (out)")
-        out = torch.empty(V, D, dtype=dout.dtype if dtype is None else dtype, device=dout.device)
-    _same("out", out, dout, (V, D))
-    p = make_embed_params(ids.numel(), D, V, out.dtype, dout.dtype, scale, accumulate)
+        out = dout.new_empty((V, D), dtype=dout.dtype if dtype is None else dtype)
+    p = BdlmEmbedParams(ids.numel(), D, V, DTYPES[out.dtype], DTYPES[dout.dtype], scale, 1 if accumulate else 0)
+    at = ctypes.byref(p)
     if workspace is None:
-        workspace = torch.empty(max(bdlm_embed_workspace_bytes(p), 16), dtype=torch.uint8, device=dout.device)
-    rc = lib().bdlm_embed_bwd(ctypes.byref(p), _ptr(dout), _ptr(ids), _ptr(out), _ptr(workspace), workspace.numel(), _stream())
+        workspace = dout.new_empty(max(lib().bdlm_embed_workspace_bytes(at), 16), dtype=torch.uint8)
+    rc = lib().bdlm_embed_bwd(at, _checked("dout", dout, shape, dout.dtype, index), ids_at, _checked("out", out, (V, D), out.dtype, index),
+                              _ptr(workspace), workspace.numel(), torch._C._cuda_getCurrentRawStream(index))
     if rc != 0:
         raise BdlmError(rc, "bdlm_embed_bwd")
     return out
