@@ -237,12 +237,15 @@ int bdlm_attn_bwd_packed(const bdlm_params* p, const bdlm_packed_geometry* g,
  *     reproducibility are those of bdlm_attn_fwd_packed / bdlm_attn_bwd_packed (bdlm_workspace_bytes_packed).
  */
 typedef struct {
-  const int32_t* table;   /* device, [L + 1][2] int32, 8-byte aligned, as bdlm_doc_table wrote it */
+  const int32_t* table;   /* device, bdlm_doc_table_bytes(L), 8-byte aligned, as bdlm_doc_table wrote it */
   int32_t max_len;        /* tokens of the longest document; chooses launch shapes, never results' meaning.  0 = not known */
   int32_t reserved;       /* 0 */
   int64_t pairs;          /* sum of n (n + 1) / 2 over the documents' lengths n; likewise.  0 = not known */
 } bdlm_docs;
 
+/* Bytes of a table for L positions (0 for an invalid L): first position and end of each position's document, [L + 1][2] int32,
+ * and the orders in which calls start their tiles. */
+size_t bdlm_doc_table_bytes(int32_t L);
 int bdlm_doc_table(const int32_t* cu_seqlens, int32_t n_docs, int32_t L, int32_t* table, void* cuda_stream);
 
 int bdlm_attn_fwd_docs(const bdlm_params* p, const bdlm_packed_geometry* g, const bdlm_docs* docs,

@@ -24,7 +24,7 @@ EXPORTS = ("bdlm_workspace_bytes", "bdlm_attn_fwd", "bdlm_attn_bwd", "bdlm_lse_m
            "bdlm_status_string", "bdlm_get_device_status", "bdlm_set_trace_buffer",
            "bdlm_attn_bwd_static_scratch", "bdlm_workspace_bytes_packed", "bdlm_attn_fwd_packed",
            "bdlm_attn_bwd_packed", "bdlm_selftest_wait_timeout", "bdlm_linear_ce_workspace_bytes",
-           "bdlm_linear_ce_fwd", "bdlm_linear_ce_bwd", "bdlm_doc_table", "bdlm_attn_fwd_docs", "bdlm_attn_bwd_docs",
+           "bdlm_linear_ce_fwd", "bdlm_linear_ce_bwd", "bdlm_doc_table", "bdlm_doc_table_bytes", "bdlm_attn_fwd_docs", "bdlm_attn_bwd_docs",
            "bdlm_norm_workspace_bytes", "bdlm_norm_fwd", "bdlm_norm_bwd", "bdlm_embed_workspace_bytes", "bdlm_embed_fwd",
            "bdlm_embed_bwd")
 LCE_WS_FWD, LCE_WS_BWD, LCE_WS_FWD_LEAST, LCE_WS_BWD_LEAST = 0, 1, 2, 3
@@ -112,6 +112,8 @@ def lib():
         L.bdlm_attn_bwd_packed.restype = ctypes.c_int
         L.bdlm_attn_bwd_packed.argtypes = [pp, gp] + [vp] * 18 + [vp, ctypes.c_size_t, vp]
         dp = ctypes.POINTER(BdlmDocs)
+        L.bdlm_doc_table_bytes.restype = ctypes.c_size_t
+        L.bdlm_doc_table_bytes.argtypes = [ctypes.c_int32]
         L.bdlm_doc_table.restype = ctypes.c_int
         L.bdlm_doc_table.argtypes = [vp, ctypes.c_int32, ctypes.c_int32, vp, vp]
         L.bdlm_attn_fwd_docs.restype = ctypes.c_int
@@ -363,12 +365,13 @@ def _packed_setup(q_clean, k_clean, q_noisy, block_size, block_prefix, clean_q_p
 
 
 class DocTable:
-    """The table of a packed batch's documents (bdlm_doc_table): `table` int32 [L + 1, 2] on the device, `struct` what the
-    library is handed.  One table serves every layer's forward and backward of the batch."""
+    """The table of a packed batch's documents (bdlm_doc_table): `table` int32 [L + 1, 2] on the device (each position's
+    document), `struct` what the library is handed.  One table serves every layer's forward and backward of the batch."""
 
-    def __init__(self, table, L, max_len, pairs):
-        self.table, self.L, self.max_len, self.pairs = table, L, max_len, pairs
-        self.struct = BdlmDocs(table.data_ptr(), max_len, 0, pairs)
+    def __init__(self, buffer, L, max_len, pairs):
+        self.buffer, self.L, self.max_len, self.pairs = buffer, L, max_len, pairs
+        self.table = buffer[:2 * (L + 1)].view(L + 1, 2)
+        self.struct = BdlmDocs(buffer.data_ptr(), max_len, 0, pairs)
 
 
 def bdlm_doc_table(cu_seqlens, L=None, device=None) -> DocTable:
@@ -389,11 +392,11 @@ def bdlm_doc_table(cu_seqlens, L=None, device=None) -> DocTable:
         raise ValueError("L must lie in [1, 2**30]")
     with torch.cuda.device(device):
         dev = cu.to(device=device, dtype=torch.int32).contiguous()
-        table = torch.empty(L + 1, 2, dtype=torch.int32, device=device)
-        rc = lib().bdlm_doc_table(_ptr(dev), dev.numel() - 1, L, _ptr(table), _stream())
+        buffer = torch.empty(lib().bdlm_doc_table_bytes(L) // 4, dtype=torch.int32, device=device)
+        rc = lib().bdlm_doc_table(_ptr(dev), dev.numel() - 1, L, _ptr(buffer), _stream())
     if rc != 0:
         raise BdlmError(rc, "bdlm_doc_table")
-    return DocTable(table, L, int(lens.max()), int((lens * (lens + 1) // 2).sum()))
+    return DocTable(buffer, L, int(lens.max()), int((lens * (lens + 1) // 2).sum()))
 
 
 def _check_docs(docs, k_clean, kv_chunks):

@@ -79,6 +79,8 @@ void fill(KArgs& a, const bdlm_params* p, const bdlm_packed_geometry* g, const b
   a.docs = docs != nullptr ? reinterpret_cast<const int2*>(docs->table) : nullptr;
   a.doc_max = docs != nullptr ? (docs->max_len > 0 && docs->max_len < p->L ? docs->max_len : p->L) : 0;
   a.doc_pairs = docs != nullptr ? (double)docs->pairs : 0;
+  for (int w = 0; w < DOC_ORDERS; ++w)
+    a.doc_order[w] = docs != nullptr && doc_tiles(p->L, KEYS_128) <= DOC_ORDER_MOST ? docs->table + doc_order_offset(p->L, w) : nullptr;
   a.scale = p->scale > 0.f ? p->scale : 1.0f / sqrtf((float)p->d);
   a.scale_log2 = a.scale * LOG2E;
   a.mode = p->clean_mask_mode;
@@ -296,6 +298,8 @@ int bdlm_attn_bwd_packed(const bdlm_params* p, const bdlm_packed_geometry* g,
                   lse_noisy, do_clean, do_noisy, dq_clean, dk_clean, dv_clean, dq_noisy, dk_noisy, dv_noisy,
                   workspace, workspace_bytes, cuda_stream);
 }
+
+size_t bdlm_doc_table_bytes(int32_t L) { return L <= 0 || L > (1 << 30) ? 0 : (size_t)doc_table_ints(L) * sizeof(int32_t); }
 
 int bdlm_doc_table(const int32_t* cu_seqlens, int32_t n_docs, int32_t L, int32_t* table, void* cuda_stream) {
   if (n_docs <= 0 || L <= 0 || L > (1 << 30) || cu_seqlens == nullptr || table == nullptr) return BDLM_ERR_INVALID_ARG;

@@ -37,6 +37,7 @@ struct KArgs {
   const int2* docs;
   int doc_max;
   double doc_pairs;
+  const int* doc_order[3];   // the tiles (DocOrder) from the most work down, nullptr: not known
   float scale;        // q.k multiplier (1/sqrt(d) by default)
   float scale_log2;   // scale * log2(e): scores are exponentiated with exp2
   int mode;           // clean_mask_mode
@@ -165,13 +166,39 @@ int device_sm_count();
 //                    the ideal duration of the launch (short sequences; dispatch_rules.h), where the first order would
 //                    start the heavy tiles of the second and later batch elements too late.
 // parts: CTAs that share one unit (the backward's key tiles: a cluster of that size), index i = unit * parts + part.
-struct TileGrid { int nx, ny, nz, tile_major, parts; };
+// order: with packed documents the work of a tile follows its place in its document; the x-th heaviest tile is order[x] then
+// (tile-major orders only).
+struct TileGrid { int nx, ny, nz, tile_major, parts; const int* order; };
 __device__ __forceinline__ void tile_grid_decode(const TileGrid& g, int i, int& x, int& y, int& z) {
   if (!g.tile_major) { x = i % g.nx; i /= g.nx; y = i % g.ny; z = i / g.ny; }
   else { const int c = g.ny * g.nz; x = i / c; i -= x * c; y = i % g.ny; z = i / g.ny; }
+  if (g.order != nullptr) x = __ldg(g.order + x);
 }
+// The order of the tiles of the clean positions, where the launch's tiles are those: all positions have queries, and the
+// noisy blocks, if any, are the sequence's.
+inline const int* doc_order(const KArgs& a, int nx, int which);
 inline TileGrid make_tile_grid(int nx, int ny, int nz) {   // one CTA per unit, one on an SM
-  return {nx, ny, nz, tile_major_pays(nx, ny, nz, nx, device_sm_count(), ORDER_RATIO) ? 1 : 0, 1};
+  return {nx, ny, nz, tile_major_pays(nx, ny, nz, nx, device_sm_count(), ORDER_RATIO) ? 1 : 0, 1, nullptr};
+}
+// Tiles of the clean positions whose orders a table of documents holds (queries counted from the last tile down, as the
+// forward's and the dQ pass's x is).
+enum DocOrder { KEYS_128, QUERIES_128, QUERIES_256 };
+constexpr int DOC_ORDERS = 3;
+constexpr int DOC_ORDER_MOST = 4096;   // tiles of 128 positions: longer launches are never tile-major
+__host__ __device__ inline int doc_tiles(int L, int which) { const int rows = which == QUERIES_256 ? 256 : 128; return (L + rows - 1) / rows; }
+// The same for a call that may be over packed documents; `stacks` of them have work.
+inline TileGrid make_doc_grid(const KArgs& a, int nx, int ny, int nz, int stacks, DocOrder which, double ratio) {
+  TileGrid tg = make_tile_grid(nx, ny, nz);
+  const double rows = which == QUERIES_256 ? 256 : 128;
+  if (a.docs == nullptr || !doc_order_pays(a.doc_max / rows + 1, a.doc_pairs, rows, nx, stacks, device_sm_count(), ratio)) return tg;
+  tg.order = doc_order(a, nx, which);
+  if (tg.order != nullptr) tg.tile_major = 1;
+  return tg;
+}
+inline const int* doc_order(const KArgs& a, int nx, int which) {
+  if (a.q[CLEAN] != nullptr ? a.cq_pos0 != 0 || a.Lqc != a.L : true) return nullptr;
+  if ((a.q[NOISY] != nullptr && a.Ln != a.L) || nx != doc_tiles(a.L, which)) return nullptr;
+  return a.doc_order[which];
 }
 // Number of CTAs, or 0 if it does not fit a grid dimension.
 inline unsigned tile_grid_blocks(const TileGrid& g) {
@@ -227,6 +254,13 @@ cudaError_t launch_portable_bwd(const KArgs& a, int passes, cudaStream_t st);
 cudaError_t launch_bwd_prepare(const KArgs& a, float* dsum_clean, float* dsum_noisy, bool zero_dq, cudaStream_t st);
 // The table of documents (bdlm_doc_table).
 cudaError_t launch_doc_table(const int* cu_seqlens, int n_docs, int L, int2* table, cudaStream_t st);
+// Its int32 after the table itself: the orders, one after the other (none for more than DOC_ORDER_MOST tiles).
+inline int64_t doc_order_offset(int L, int which) {
+  int64_t at = 2 * ((int64_t)L + 1);
+  for (int w = 0; w < which; ++w) at += doc_tiles(L, w);
+  return at;
+}
+inline int64_t doc_table_ints(int L) { return doc_order_offset(L, doc_tiles(L, KEYS_128) <= DOC_ORDER_MOST ? DOC_ORDERS : 0); }
 cudaError_t launch_merge(int n, int batch, int L, int H, int d, const void* const* o_parts,
                          const float* const* lse_parts, int dtype, void* o_out, float* lse_out,
                          cudaStream_t st);

@@ -20,6 +20,23 @@ inline bool tile_major_pays(int nx, int ny, int nz, double heavy, int at_once, d
   const double stack = heavy * nx - heavy * (heavy - 1) / 2;
   return heavy * ratio * at_once > stack * ny * nz;
 }
+// Packed documents: whether the tiles of the launch start from the heaviest down, documents mixed.  `heavy` tiles of `rows`
+// positions the longest document has, `pairs` visible pairs there are (0: not known) in the nx tiles of a stack.  The forward
+// gains wherever the heaviest unit takes more than 1 / DOC_RATIO_FWD of the launch; the backward only where it takes more than an
+// SM's share, because neighbouring tiles walk the same queries, and the same dQ accumulators, together.  Documents in their
+// order / mixed (us), by the heaviest unit over an SM's share in the backward:
+//            1.37   8000 tokens: 3000, 3000, 2000, H = 16 / 4                   forward  119 / 106     backward  321 /  311
+//            1.21   5500 tokens: 6 documents of 100 to 2000, H = 24 / 8                   76 /  72               210 /  192
+//            1.18   8 x 1000, H = 12 / 4, d = 64                                          48 /  46               122 /   94
+//            1.09   4 x 2048, H = 16 / 4, d = 64                                          67 /  65               207 /  161
+//            0.86   8192 tokens: 6 of 64 to 3200, H = 32 / 8, noisy blocks too           350 / 300               959 / 1025
+//            0.55   4 x 2048, H = 32 / 8                                                 129 / 129               429 /  461
+//            0.48   16384 tokens: 12 of 17 to 4096, H = 32 / 8                           385 / 360              1131 / 1174
+constexpr double DOC_RATIO_FWD = 5, DOC_RATIO_BWD = 1;
+inline bool doc_order_pays(double heavy, double pairs, double rows, int nx, int stacks, int at_once, double ratio) {
+  const double stack = pairs > 0 ? pairs / (rows * rows) + 0.5 * nx : 0.5 * heavy * nx;
+  return heavy * ratio * at_once > stack * stacks;
+}
 constexpr double ORDER_RATIO = 5;   // one CTA per tile: 10 SMs > ny nz (nx + 1)
 
 // Pairs of CTAs (backward): half as many units at once, each of 256 keys.  Measured x-fastest / tile-major, sustained at the

@@ -207,11 +207,47 @@ __global__ void __launch_bounds__(256) doc_table_kernel(const int* __restrict__ 
   table[p] = a <= p && p < z ? make_int2(a, z) : make_int2((int)p, (int)p);
 }
 
+// The order of the tiles of one kind (blockIdx.y, a DocOrder), the most work first: a tile's rank is the number of tiles that
+// come before it, counted.  Work: the rows that see a key tile, or the keys that a query tile sees.
+__global__ void __launch_bounds__(256) doc_order_kernel(const int2* table, int L, int* keys_128, int* queries_128, int* queries_256) {
+  __shared__ int work[DOC_ORDER_MOST];
+  wait_for_predecessor();
+  const int which = blockIdx.y, rows = which == QUERIES_256 ? 256 : 128, n = doc_tiles(L, which);
+  const bool queries = which != KEYS_128;
+  if ((int)blockIdx.x * 256 >= n) return;
+  for (int t = threadIdx.x; t < n; t += 256) {
+    const int first = t * rows, last = min(L, first + rows) - 1;
+    work[t] = queries ? last + 1 - table[first].x : table[last].y - first;
+  }
+  __syncthreads();
+  const int t = blockIdx.x * 256 + threadIdx.x;
+  if (t >= n) return;
+  int rank = 0;
+#pragma unroll 8
+  for (int u = 0; u < n; ++u) rank += work[u] > work[t] || (work[u] == work[t] && u < t);
+  int* order = which == KEYS_128 ? keys_128 : which == QUERIES_128 ? queries_128 : queries_256;
+  order[rank] = queries ? n - 1 - t : t;
+}
+
 }  // namespace
 
 cudaError_t launch_doc_table(const int* cu_seqlens, int n_docs, int L, int2* table, cudaStream_t st) {
   doc_table_kernel<<<(unsigned)(((int64_t)L + 256) / 256), 256, 0, st>>>(cu_seqlens, n_docs, L, table);
-  return cudaGetLastError();
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess || doc_tiles(L, KEYS_128) > DOC_ORDER_MOST) return e;
+  int* at = reinterpret_cast<int*>(table);
+  int* order[DOC_ORDERS];
+  for (int w = 0; w < DOC_ORDERS; ++w) order[w] = at + doc_order_offset(L, w);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((doc_tiles(L, KEYS_128) + 255) / 256, DOC_ORDERS);
+  cfg.blockDim = dim3(256);
+  cfg.stream = st;
+  cudaLaunchAttribute attr = {};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, doc_order_kernel, (const int2*)table, L, order[0], order[1], order[2]);
 }
 
 cudaError_t launch_merge(int n, int batch, int L, int H, int d, const void* const* o_parts,

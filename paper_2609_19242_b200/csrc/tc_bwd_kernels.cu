@@ -1385,7 +1385,7 @@ static cudaError_t launch_tc_bwd_d(const KArgs& a, int passes, cudaStream_t st) 
         if ((e = launch_tc_bwd_pair(a, true, st, after_rows)) != cudaSuccess) return e;
       } else {
         auto kern = a.trace ? tc_bwdf_kernel<true, D> : tc_bwdf_kernel<false, D>;
-        TileGrid tg = make_tile_grid((max(a.L, a.k[NOISY] != nullptr ? a.Ln : 0) + TILE - 1) / TILE, a.Hkv, a.batch * 2);
+        TileGrid tg = make_doc_grid(a, (max(a.L, a.k[NOISY] != nullptr ? a.Ln : 0) + TILE - 1) / TILE, a.Hkv, a.batch * 2, a.Hkv * a.batch, KEYS_128, DOC_RATIO_BWD);
         tg.parts = parts;
         if ((e = launch_units(kern, tg, BF_THREADS, BF_SMEM, st, maps, a, status, after_rows)) != cudaSuccess) return e;
       }
@@ -1408,13 +1408,14 @@ static cudaError_t launch_tc_bwd_d(const KArgs& a, int passes, cudaStream_t st) 
       if ((e = launch_tc_bwd_pair(a, false, st, after_rows)) != cudaSuccess) return e;
     } else {
       auto kern = a.trace ? tc_dkdv_kernel<true, D> : tc_dkdv_kernel<false, D>;
-      const TileGrid tg = make_tile_grid((max(a.L, a.k[NOISY] != nullptr ? a.Ln : 0) + TILE - 1) / TILE, a.Hkv, a.batch * 2);
+      const TileGrid tg = make_doc_grid(a, (max(a.L, a.k[NOISY] != nullptr ? a.Ln : 0) + TILE - 1) / TILE, a.Hkv, a.batch * 2, a.Hkv * a.batch, KEYS_128, DOC_RATIO_BWD);
       if ((e = launch_units(kern, tg, DKDV_THREADS, DKDV_SMEM, st, maps, a, status, after_rows)) != cudaSuccess) return e;
     }
   }
   if (passes & BDLM_BWD_PASS_DQ) {
     auto kern = a.trace ? tc_dq_kernel<true, D> : tc_dq_kernel<false, D>;
-    const TileGrid tg = make_tile_grid((max(a.q[CLEAN] != nullptr ? a.Lqc : 0, a.q[NOISY] != nullptr ? a.Ln : 0) + TILE - 1) / TILE, a.H, a.batch * 2);
+    const TileGrid tg = make_doc_grid(a, (max(a.q[CLEAN] != nullptr ? a.Lqc : 0, a.q[NOISY] != nullptr ? a.Ln : 0) + TILE - 1) / TILE, a.H, a.batch * 2,
+                                      a.H * a.batch * ((a.q[CLEAN] != nullptr) + (a.q[NOISY] != nullptr)), QUERIES_128, DOC_RATIO_FWD);
     // (chained to whichever of this call's kernels came before)
     if ((e = launch_units(kern, tg, BWD_THREADS, DQ_SMEM, st, maps, a, status, (passes & (BDLM_BWD_PASS_DSUM | BDLM_BWD_PASS_DKDV)) != 0)) != cudaSuccess) return e;
   }

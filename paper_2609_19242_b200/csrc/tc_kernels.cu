@@ -565,7 +565,7 @@ static cudaError_t launch_tc_fwd_d(const KArgs& a, cudaStream_t st) {
     auto kern = a.trace ? tc_fwdr_kernel<true, false, D> : tc_fwdr_kernel<false, false, D>;
     e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, FWDR_SMEM);
     if (e != cudaSuccess) return e;
-    const TileGrid tg = make_tile_grid((qrows + TILE - 1) / TILE, a.H / 2, a.batch * streams);
+    const TileGrid tg = make_doc_grid(a, (qrows + TILE - 1) / TILE, a.H / 2, a.batch * streams, a.H / 2 * a.batch * streams, QUERIES_128, DOC_RATIO_FWD);
     if (tile_grid_blocks(tg) == 0) return cudaErrorInvalidValue;
     kern<<<tile_grid_blocks(tg), FWDR_THREADS, FWDR_SMEM, st>>>(maps, a, tg, status);
     return cudaGetLastError();
@@ -574,7 +574,7 @@ static cudaError_t launch_tc_fwd_d(const KArgs& a, cudaStream_t st) {
   auto kern = a.trace ? tc_fwdr_kernel<true, true, D> : tc_fwdr_kernel<false, true, D>;
   e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, FWDR_SMEM);
   if (e != cudaSuccess) return e;
-  const TileGrid tg = make_tile_grid(((qrows + TILE - 1) / TILE + 1) / 2, a.H, a.batch * streams);
+  const TileGrid tg = make_doc_grid(a, ((qrows + TILE - 1) / TILE + 1) / 2, a.H, a.batch * streams, a.H * a.batch * streams, QUERIES_256, DOC_RATIO_FWD);
   if (tile_grid_blocks(tg) == 0) return cudaErrorInvalidValue;
   kern<<<tile_grid_blocks(tg), FWDR_THREADS, FWDR_SMEM, st>>>(maps, a, tg, status);
   return cudaGetLastError();

@@ -250,9 +250,27 @@ def test_table_of_documents():
 def test_wrong_tables_stay_inside_the_tensors():
     """The library does not validate the entries on the device: wrong ones give wrong documents inside [0, L]."""
     cu = torch.tensor([50, 20, -7, 2 ** 31 - 1, 90], dtype=torch.int32, device="cuda")
-    table = torch.empty(65, 2, dtype=torch.int32, device="cuda")
-    assert binding.lib().bdlm_doc_table(cu.data_ptr(), 4, 64, table.data_ptr(), binding._stream()) == 0
-    assert int(table.min()) >= 0 and int(table.max()) <= 64
+    buffer = torch.full((binding.lib().bdlm_doc_table_bytes(64) // 4,), -1, dtype=torch.int32, device="cuda")
+    assert binding.lib().bdlm_doc_table(cu.data_ptr(), 4, 64, buffer.data_ptr(), binding._stream()) == 0
+    assert int(buffer.min()) >= 0 and int(buffer[:130].max()) <= 64 and (buffer[130:] == 0).all()   # one tile of each kind
+
+
+def test_order_of_tiles():
+    """The orders behind the table are the tiles by the work that they have, ties by place."""
+    rng = np.random.default_rng(4)
+    for lens in ([1000, 3, 700, 128, 128, 2000], list(rng.integers(1, 400, size=60)), [5]):
+        cu = np.concatenate([[0], np.cumsum(lens)])
+        L = int(cu[-1])
+        docs = binding.bdlm_doc_table([int(c) for c in cu])
+        begin, end = docs.table[:, 0].cpu().numpy(), docs.table[:, 1].cpu().numpy()
+        at = 2 * (L + 1)
+        for rows, queries in ((128, False), (128, True), (256, True)):
+            n = -(-L // rows)
+            work = [min(L, (t + 1) * rows) - begin[t * rows] if queries else end[min(L, (t + 1) * rows) - 1] - t * rows for t in range(n)]
+            want = sorted(range(n), key=lambda t: (-work[t], t))
+            assert docs.buffer[at:at + n].tolist() == [n - 1 - t if queries else t for t in want]
+            at += n
+        assert at == docs.buffer.numel()
 
 
 def test_refusals():
