@@ -236,6 +236,57 @@ def test_reproducible_two_pass_gradients_and_capture():
             assert torch.equal(a, b)
 
 
+def test_shards_of_the_keys_merge_to_the_whole():
+    """Context shards cut across documents; a shard without a row's document leaves the row empty."""
+    t, g, _ = _inputs(640, 640, 640, 4, 2, 128)
+    docs = binding.bdlm_doc_table([0, 96, 128, 480, 640])
+    qkv = [g[n] for n in ("q_clean", "k_clean", "v_clean", "q_noisy", "k_noisy", "v_noisy")]
+    whole = binding.bdlm_attn_fwd_packed(*qkv, 32, docs=docs)
+    parts = [binding.bdlm_attn_fwd_packed(*qkv, 32, docs=docs, kv_range=r, include_noisy_diag=diag)
+             for r, diag in (((0, 100), True), ((100, 300), False), ((300, 300), False), ((300, 640), False))]
+    assert torch.isneginf(parts[0][1][:, :, 480:]).all() and (parts[0][0][:, 480:] == 0).all()
+    for s in (0, 2):
+        o, lse = binding.bdlm_lse_merge([x[s] for x in parts], [x[s + 1] for x in parts])
+        assert float((lse - whole[s + 1]).abs().max()) <= 1e-4
+        # each partial output and the merged one are rounded: 2^-8 of the value each, the weights sum to one
+        assert float((o.float() - whole[s].float()).abs().max()) <= 3 * 2.0 ** -8 * float(whole[s].float().abs().max())
+
+
+def test_scale_and_passes_one_by_one():
+    t, g, _ = _inputs(300, 300, 0, 4, 2, 64)
+    docs = binding.bdlm_doc_table([0, 130, 300])
+    qkv = [g[n] for n in ("q_clean", "k_clean", "v_clean")] + [None] * 3
+    doubled = [(g["q_clean"].float() * 2).bfloat16()] + qkv[1:]
+    out = binding.bdlm_attn_fwd_packed(*qkv, 1, docs=docs, scale=0.25)          # 64 ** -0.5 = 0.125
+    twice = binding.bdlm_attn_fwd_packed(*doubled, 1, docs=docs)
+    assert torch.equal(out[0], twice[0]) and torch.equal(out[1], twice[1])
+    args = (*qkv, *out, g["do_clean"], None, 1)
+    want = binding.bdlm_attn_bwd_packed(*args, docs=docs, scale=0.25, single_pass=False)
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    got = tuple(torch.empty_like(x) for x in want[:3]) + (None,) * 3
+    for one in (binding.PASS_DSUM, binding.PASS_DKDV, binding.PASS_DQ):
+        binding.bdlm_attn_bwd_packed(*args, docs=docs, scale=0.25, single_pass=False, passes=one, workspace=ws, out=got)
+    for a, b in zip(got[:3], want[:3]):
+        assert torch.equal(a, b)
+
+
+def test_tables_on_two_streams():
+    """A table made on one stream and used on others after an event, with calls of different documents at once."""
+    t, g, _ = _inputs(512, 512, 0, 4, 2, 64)
+    qkv = [g[n] for n in ("q_clean", "k_clean", "v_clean")] + [None] * 3
+    tables = [binding.bdlm_doc_table(cu) for cu in ([0, 200, 512], [0, 1, 300, 301, 512])]
+    want = [binding.bdlm_attn_fwd_packed(*qkv, 1, docs=d)[0].clone() for d in tables]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in tables], []
+    for _ in range(4):
+        for s, d in zip(streams, tables):
+            with torch.cuda.stream(s):
+                got.append(binding.bdlm_attn_fwd_packed(*qkv, 1, docs=d)[0])
+    torch.cuda.synchronize()
+    for i, o in enumerate(got):
+        assert torch.equal(o, want[i % 2])
+
+
 def test_table_of_documents():
     for cu, L in (([0, 4, 4, 9], 9), ([2, 5, 6], 8), ([0, 1], 1), ([3, 3, 3], 5)):
         table = binding.bdlm_doc_table(torch.tensor(cu, dtype=torch.int32, device="cuda"), L)

@@ -154,6 +154,31 @@ def test_many_tokens():
     _check_bwd(70001, 16, 3000, masked=0.5)
 
 
+def test_more_elements_than_32_bits_count():
+    """Tables and rows of tokens past 2^31 elements."""
+    V, D = 524288 + 100, 4096
+    table = torch.zeros(V, D, device="cuda", dtype=BF16)
+    table[-5:] = torch.randn(5, D, device="cuda").to(BF16)
+    ids = torch.tensor([V - 1, 0, V - 5, V, V - 3], dtype=torch.int32, device="cuda")
+    out = binding.bdlm_embed_fwd(table, ids)
+    for t, v in ((0, V - 1), (1, 0), (2, V - 5), (4, V - 3)):
+        assert torch.equal(out[t], table[v])
+    assert (out[3] == 0).all()
+    grad = binding.bdlm_embed_bwd(out, ids, V, out=table)
+    want = {V - 1: 0, V - 5: 2, V - 3: 4}
+    for v in (V - 1, V - 2, V - 3, V - 4, V - 5):
+        assert torch.equal(grad[v], out[want[v]]) if v in want else (grad[v] == 0).all()
+    assert (grad[:-5] == 0).all()
+    del table, grad
+    T, D = 1 << 20, 2056
+    dout = torch.ones(T, D, device="cuda", dtype=BF16)
+    dout[:-8] = 0
+    ids = torch.full((T,), 2, dtype=torch.int32, device="cuda")
+    ids[-3:] = 1
+    grad = binding.bdlm_embed_bwd(dout, ids, 3, dtype=BF16)
+    assert (grad[0] == 0).all() and (grad[1] == 3).all() and (grad[2] == 5).all()
+
+
 def test_no_tokens():
     table = torch.randn(10, 16, device="cuda").to(BF16)
     ids = torch.empty(0, dtype=torch.int32, device="cuda")

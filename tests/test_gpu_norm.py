@@ -143,6 +143,30 @@ def test_mean_far_from_zero_and_constant_rows():
     assert (rstd - 100).abs().max() < 1e-3
 
 
+def test_more_elements_than_32_bits_count():
+    """2^31 elements lie before the last rows: those are the same as in a call of their own."""
+    T, D, tail = 524288 + 300, 4096, 400
+    x = torch.empty(T, D, device="cuda", dtype=BF16)
+    i = _inputs(tail, D, BF16, BF16)
+    x[:-tail] = 1.0
+    x[-tail:] = i["x"]
+    out = binding.bdlm_norm_fwd(x, i["w"], i["b"])
+    want = binding.bdlm_norm_fwd(i["x"], i["w"], i["b"])
+    for a, b in ((out[0], want[0]), (out[2], want[2]), (out[3], want[3])):
+        assert torch.equal(a[-tail:], b)
+    del out
+    mean, rstd = torch.cat([torch.zeros(T - tail, device="cuda"), want[2]]), torch.cat([torch.ones(T - tail, device="cuda"), want[3]])
+    dy = torch.zeros_like(x)
+    dy[-tail:] = i["dy"]
+    got = binding.bdlm_norm_bwd(dy, x, i["w"], mean, rstd, bias=True)
+    ref = binding.bdlm_norm_bwd(i["dy"], i["x"], i["w"], want[2], want[3], bias=True)
+    assert torch.equal(got[0][-tail:], ref[0]) and (got[0][:-tail] == 0).all()
+    # the same sums in another order of rows
+    for a, b, size in ((got[1], ref[1], (i["dy"].float() * (i["x"].float() - want[2][:, None]) * want[3][:, None]).abs().sum(0)),
+                       (got[2], ref[2], i["dy"].float().abs().sum(0))):
+        assert ((a.float() - b.float()).abs() <= 2.0 ** -7 * b.float().abs() + 2 * tail * 2.0 ** -24 * size).all()
+
+
 def test_no_rows():
     x = torch.empty(0, 64, device="cuda", dtype=BF16)
     w = torch.ones(64, device="cuda", dtype=BF16)
