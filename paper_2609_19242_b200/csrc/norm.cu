@@ -37,6 +37,8 @@ __host__ __device__ constexpr int bwd_items(int V) { return 16 / V; }
 __host__ __device__ constexpr bool fwd_long(int items, Span s) { return s != NARROW && items == 4; }
 constexpr int NARROW_THREADS = 128, BWD_THREADS = 512;   // of a CTA, at most
 __host__ __device__ constexpr int fwd_threads(int V, int items, Span s) { return s == NARROW ? NARROW_THREADS : fwd_long(items, s) && V == 4 ? 1024 : 512; }
+// (64 registers where a row takes a CTA: 16384 x 4095 forward 242 us with 99, 144 with these)
+__host__ __device__ constexpr int fwd_ctas(int items, Span s) { return s == WIDE && items == 2 ? 2 : s == NARROW ? (items == 4 ? 4 : 8) : 1; }
 // Rows in flight in the backward: the same number of bytes for 16- and 32-bit elements.
 __host__ __device__ constexpr int ring_of(int V) { return V == 8 ? 4 : 2; }
 
@@ -185,7 +187,7 @@ constexpr int RED_FLOATS = 2 * 32 * 2;   // two buffers in turn, 32 warps, two s
 // The forward loads a row's vectors straight into registers: a thread has nothing else to keep, so four CTAs of a 4096-element
 // row share an SM and their loads lie under one another.  (The backward's ring took 101 us here instead of 89, 16384 x 4096.)
 template <class T, class W, int V, int ITEMS, Span S, bool SHIFT>
-__global__ void __launch_bounds__(fwd_threads(V, ITEMS, S)) norm_fwd_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(fwd_threads(V, ITEMS, S), fwd_ctas(ITEMS, S)) norm_fwd_kernel(const NormArgs a) {
   constexpr bool LONG = fwd_long(ITEMS, S);
   __shared__ float red[RED_FLOATS];
   const int tpr = S == NARROW ? a.tpr : (int)blockDim.x, lane = S == NARROW ? (int)threadIdx.x % tpr : (int)threadIdx.x;
@@ -316,7 +318,8 @@ __global__ void __launch_bounds__(fwd_threads(V, ITEMS, S)) norm_fwd_kernel(cons
 }
 
 // The products of a row's elements are packed two to an instruction: at 20 instructions an element, which they took one by one,
-// their issue was as long as the memory's time (16384 x 4096 bf16: MEASURED).
+// their issue took as long as the memory does (16384 x 4096 bf16: 101 us, now 93 with the reduction, of which the memory's
+// rate would allow 82).
 template <class T, class W, int V, int ITEMS, Span S, bool SHIFT>
 __global__ void __launch_bounds__(BWD_THREADS) norm_bwd_kernel(const NormArgs a) {
   constexpr int RING = ring_of(V);
