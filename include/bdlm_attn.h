@@ -230,8 +230,10 @@ int bdlm_attn_bwd_packed(const bdlm_params* p, const bdlm_packed_geometry* g,
  *     backward, share it.  It is the same for all batch elements.  cu_seqlens is a DEVICE array of n_docs + 1
  *     non-decreasing int32 in [0, L] (empty documents are allowed); its values are not validated, wrong ones give wrong
  *     masks but no access outside the tensors.  Positions before the first and from the last entry on belong to no document:
- *     clean rows there see nothing (O = 0, LSE = -inf, zero gradients), but like all rows they have to hold finite values,
- *     because the products run over whole tiles.
+ *     clean rows there see nothing (O = 0, LSE = -inf, zero gradients).
+ *   - Finite values of one document have no effect on another, but the products run over whole tiles, and there a hidden zero
+ *     times a NaN or an infinity is NaN: from one document, or from positions of none, it can reach rows of its neighbours up to 256
+ *     positions away.  All rows have to hold finite values.
  *   - With q_noisy NULL this is causal attention over prompts of different lengths (block_size is then unused: pass 1).
  *   - kv_chunk_len > 0 is not offered together with documents (BDLM_ERR_UNSUPPORTED).  Workspace, statuses, layouts and
  *     reproducibility are those of bdlm_attn_fwd_packed / bdlm_attn_bwd_packed (bdlm_workspace_bytes_packed).

@@ -16,7 +16,7 @@
  *   table, dtable   [V, D]  of `table_dtype`
  *   out, dout       [T, D]  of `out_dtype`: table_dtype, or any type where table_dtype is BDLM_FP32
  *   ids             [T]     int32
- * T = 0 is a call without tokens (dtable becomes zero, or stays as it is with accumulate = 1).
+ * No output overlaps an input.  T = 0 is a call without tokens (dtable becomes zero, or stays as it is with accumulate = 1).
  */
 #ifndef BDLM_EMBED_H_
 #define BDLM_EMBED_H_

@@ -29,7 +29,14 @@ EXPORTS = ("bdlm_workspace_bytes", "bdlm_attn_fwd", "bdlm_attn_bwd", "bdlm_lse_m
            "bdlm_embed_bwd")
 LCE_WS_FWD, LCE_WS_BWD, LCE_WS_FWD_LEAST, LCE_WS_BWD_LEAST = 0, 1, 2, 3
 NORM_LAYER, NORM_RMS, NORM_MAX_D = 0, 1, 32768
-DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+
+
+class _Dtypes(dict):
+    def __missing__(self, dtype):
+        raise ValueError(f"tensors of {dtype} are not supported: bf16, fp16 and fp32 are")
+
+
+DTYPES = _Dtypes({torch.bfloat16: 0, torch.float16: 1, torch.float32: 2})
 STATIC_SCRATCH_ROWS = 1 << 20
 TRACE_SLOTS = 256
 
@@ -378,7 +385,7 @@ def bdlm_doc_table(cu_seqlens, L=None, device=None) -> DocTable:
     """Table of the documents of a packed sequence of L clean positions (default: the last entry).  `cu_seqlens`: n + 1
     non-decreasing starts and ends in [0, L], int32, or a list; document i holds positions cu_seqlens[i] ..
     cu_seqlens[i + 1] - 1, positions outside all of them see nothing.  Its values are checked here, on a host copy, so a CUDA
-    tensor makes the call wait for the device: hand over the host's."""
+    tensor makes the call wait for the device (hand over the host's), and the call belongs outside a stream's capture."""
     cu = torch.as_tensor(cu_seqlens)
     if cu.dim() != 1 or cu.numel() < 2 or cu.dtype not in (torch.int32, torch.int64):
         raise ValueError("cu_seqlens must be one-dimensional int32 (or int64) with at least two entries")

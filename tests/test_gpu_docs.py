@@ -124,7 +124,7 @@ PATHS = [(AUTO, True), (AUTO, False), (PORTABLE, False)]
 
 @pytest.mark.parametrize("impl,single", PATHS)
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("lens", [[1], [5], [128], [1, 1, 1], [127, 1, 129], [100, 1, 27, 128], [300, 2, 40, 0, 90], [64] * 9, [383, 257, 1]],
+@pytest.mark.parametrize("lens", [[1], [5], [128], [1, 1, 1], [127, 1, 129], [100, 1, 27, 128], [300, 2, 40, 0, 90], [64] * 9, [383, 257, 1], [1] * 200],
                          ids=lambda l: "-".join(map(str, l)))
 def test_prompts_of_different_lengths(lens, d, impl, single):
     _check(lens, d=d, impl=impl, single_pass=single)
@@ -285,6 +285,47 @@ def test_tables_on_two_streams():
     torch.cuda.synchronize()
     for i, o in enumerate(got):
         assert torch.equal(o, want[i % 2])
+
+
+@pytest.mark.parametrize("impl,single", PATHS)
+def test_blocks_that_documents_cut(impl, single):
+    """Mask mode 1, blocks counted from position 0: a document's first and last blocks are cut by its ends."""
+    lens, M = [70, 5, 1, 130, 94], 32
+    cu = np.concatenate([[0], np.cumsum(lens)])
+    L = int(cu[-1])
+    t, g, x = _inputs(L, L, 0, 2, 1, 64)
+    out, grads = _run(g, M, binding.bdlm_doc_table([int(c) for c in cu]), mode=1, impl=impl, single_pass=single)
+    none = np.zeros((1, 0, 1, 64))
+    dk, dv = np.zeros((1, L, 1, 64)), np.zeros((1, L, 1, 64))
+    for a, z in zip(cu, cu[1:]):
+        ref = orc.attn_packed(x["q_clean"][:, a:z], x["k_clean"], x["v_clean"], None, none, none, M, do_clean=x["do_clean"][:, a:z],
+                              clean_q_pos0=a, clean_mask_mode=1, kv_begin=a, kv_end=z)
+        assert np.abs(synth.to_f64(out[0][:, a:z]) - ref["o_clean"]).max() <= pu.TOL_O * max(1.0, np.abs(ref["o_clean"]).max())
+        assert np.abs(synth.to_f64(out[1][:, :, a:z]) - ref["lse_clean"]).max() <= pu.TOL_LSE
+        dk += ref["dk_clean"]
+        dv += ref["dv_clean"]
+        if z - a > 1:
+            assert pu.rel_l2(synth.to_f64(grads[0][:, a:z]), ref["dq_clean"]) <= pu.TOL_GRAD
+    assert pu.rel_l2(synth.to_f64(grads[1]), dk) <= pu.TOL_GRAD and pu.rel_l2(synth.to_f64(grads[2]), dv) <= pu.TOL_GRAD
+
+
+def test_a_captured_call_takes_the_documents_of_a_rewritten_table():
+    """The launches depend on a table's contents for their order alone: a table written again in place, for other documents of the
+    same positions, is what a replay goes by."""
+    t, g, _ = _inputs(900, 900, 0, 6, 2, 64)
+    qkv = [g[n] for n in ("q_clean", "k_clean", "v_clean")] + [None] * 3
+    docs = binding.bdlm_doc_table([0, 300, 900])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = binding.bdlm_attn_fwd_packed(*qkv, 1, docs=docs)
+        grads = binding.bdlm_attn_bwd_packed(*qkv, *out, g["do_clean"], None, 1, docs=docs, single_pass=False)
+    for cu in ([0, 900], [0, 1, 2, 700, 899, 900], [0, 300, 900]):
+        new = torch.tensor(cu, dtype=torch.int32, device="cuda")
+        assert binding.lib().bdlm_doc_table(new.data_ptr(), len(cu) - 1, 900, docs.buffer.data_ptr(), binding._stream()) == 0
+        graph.replay()
+        want, wgrads = _run(g, 1, binding.bdlm_doc_table(cu), single_pass=False)
+        for a, b in zip((*out[:2], *grads[:3]), (*want[:2], *wgrads[:3])):
+            assert torch.equal(a, b)
 
 
 def test_table_of_documents():
