@@ -40,7 +40,8 @@ typedef struct {
   int32_t reserved;      /* 0 */
 } bdlm_embed_params;
 
-/* Scratch bytes of the backward: the sorted tokens and fp32 sums of runs of equal tokens.  0 for invalid parameters. */
+/* Scratch bytes of the backward: the sorted tokens and fp32 sums of runs of equal tokens.  0 where none are needed (up to 32
+ * tokens) and for invalid parameters. */
 size_t bdlm_embed_workspace_bytes(const bdlm_embed_params* p);
 
 int bdlm_embed_fwd(const bdlm_embed_params* p, const void* table, const int32_t* ids, void* out, void* cuda_stream);

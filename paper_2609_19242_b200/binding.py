@@ -603,7 +603,7 @@ def bdlm_norm_fwd(x, weight=None, bias=None, residual=None, *, eps=1e-5, rms=Fal
     w_at, b_at = _checked("weight", weight, shape[-1:], wdtype, index), _checked("bias", bias, shape[-1:], wdtype, index)
     res_at = _checked("residual", residual, shape, dtype, index)
     if out is None:
-        y, rstd = torch.empty_like(x), x.new_empty(rows, dtype=torch.float32)
+        y, rstd = torch.empty_like(x), torch.empty(rows, dtype=torch.float32, device=x.device)
         h, mean = x if residual is None else torch.empty_like(x), None if rms else torch.empty_like(rstd)
         out = (y, h, mean, rstd)
         y_at, h_at, mean_at, rstd_at = y.data_ptr(), h.data_ptr(), None if rms else mean.data_ptr(), rstd.data_ptr()
@@ -639,7 +639,8 @@ def bdlm_norm_bwd(dy, h, weight, mean, rstd, *, dh=None, bias=False, rms=False, 
     p = BdlmNormParams(h.numel() // D if D else 0, D, DTYPES[dtype], DTYPES[wdtype], NORM_RMS if rms else NORM_LAYER)
     at = ctypes.byref(p)
     if workspace is None and (dw is not None or db is not None):
-        workspace = h.new_empty(max(lib().bdlm_norm_workspace_bytes(at), 16), dtype=torch.uint8)
+        need = lib().bdlm_norm_workspace_bytes(at)
+        workspace = torch.empty(need, dtype=torch.uint8, device=h.device) if need else None
     rc = lib().bdlm_norm_bwd(at, _checked("dy", dy, shape, dtype, index), _checked("h", h, shape, dtype, index), w_at,
                              _checked("mean", mean, rows, torch.float32, index), _checked("rstd", rstd, rows, torch.float32, index),
                              _checked("dh", dh, shape, dtype, index), dx_at, dw_at, db_at, _ptr(workspace),
@@ -667,7 +668,7 @@ def bdlm_embed_fwd(table, ids, *, scale=1.0, dtype=None, out=None):
     ids_at = _checked("ids", ids, ids.shape, torch.int32, index)
     shape = (*ids.shape, D)
     if out is None:
-        out = table.new_empty(shape, dtype=table.dtype if dtype is None else dtype)
+        out = torch.empty(shape, dtype=table.dtype if dtype is None else dtype, device=table.device)
     p = BdlmEmbedParams(ids.numel(), D, V, DTYPES[table.dtype], DTYPES[out.dtype], scale, 0)
     rc = lib().bdlm_embed_fwd(ctypes.byref(p), _ptr(table), ids_at, _checked("out", out, shape, out.dtype, index),
                               torch._C._cuda_getCurrentRawStream(index))
@@ -685,13 +686,14 @@ def bdlm_embed_bwd(dout, ids, V, *, scale=1.0, dtype=None, accumulate=False, out
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs the gradient to add to (out)")
-        out = dout.new_empty((V, D), dtype=dout.dtype if dtype is None else dtype)
+        out = torch.empty((V, D), dtype=dout.dtype if dtype is None else dtype, device=dout.device)
     p = BdlmEmbedParams(ids.numel(), D, V, DTYPES[out.dtype], DTYPES[dout.dtype], scale, 1 if accumulate else 0)
     at = ctypes.byref(p)
     if workspace is None:
-        workspace = dout.new_empty(max(lib().bdlm_embed_workspace_bytes(at), 16), dtype=torch.uint8)
+        need = lib().bdlm_embed_workspace_bytes(at)
+        workspace = torch.empty(need, dtype=torch.uint8, device=dout.device) if need else None
     rc = lib().bdlm_embed_bwd(at, _checked("dout", dout, shape, dout.dtype, index), ids_at, _checked("out", out, (V, D), out.dtype, index),
-                              _ptr(workspace), workspace.numel(), torch._C._cuda_getCurrentRawStream(index))
+                              _ptr(workspace), 0 if workspace is None else workspace.numel(), torch._C._cuda_getCurrentRawStream(index))
     if rc != 0:
         raise BdlmError(rc, "bdlm_embed_bwd")
     return out

@@ -247,7 +247,9 @@ constexpr int SUM_THREADS = 512, GROUP_THREADS = 128;   // threads of a CTA; of 
 constexpr int FILL_WORDS = 4096;                        // rows a CTA looks up at a time: a bit each
 
 // E: table, O: tokens' rows.  A group of `tpr` threads takes a piece and a slab of tpr V columns.
-template <class E, class O, int V, bool ADD>
+// FEW: no more than FEW_TOKENS of them, one piece: each CTA sorts them itself, and this is the only launch.
+constexpr int FEW_TOKENS = 32;
+template <class E, class O, int V, bool ADD, bool FEW>
 __global__ void __launch_bounds__(SUM_THREADS, 2) embed_sum_kernel(const SumArgs a) {
   __shared__ uint32_t present[FILL_WORDS];
   E* dtable = static_cast<E*>(a.dtable);
@@ -275,8 +277,24 @@ __global__ void __launch_bounds__(SUM_THREADS, 2) embed_sum_kernel(const SumArgs
       __syncthreads();
     }
   }
-  wait_for_sort();
-  let_next_start();
+  __shared__ int2 few[FEW ? FEW_TOKENS : 1];
+  if (FEW) {
+    const int lane = threadIdx.x, id = lane < a.T ? a.ids[lane] : -1, key = lane >= a.T ? 0x7fffffff : id >= 0 && id < a.V ? id : a.V;
+    if (lane < 32) {
+      int rank = 0;
+#pragma unroll
+      for (int t = 0; t < 32; ++t) {
+        const int k = __shfl_sync(0xffffffffu, key, t);
+        rank += k < key || (k == key && t < lane);
+      }
+      few[rank] = make_int2(key, lane);
+    }
+    __syncthreads();
+  } else {
+    wait_for_sort();
+    let_next_start();
+  }
+  auto pair = [&](int64_t i) { return FEW ? few[FEW ? i : 0] : __ldcg(a.sorted + i); };
   const O* dout = static_cast<const O*>(a.dout);
   const int groups = SUM_THREADS / a.tpr, lane = threadIdx.x % a.tpr;
   const int64_t items = (int64_t)a.pieces * a.slabs;
@@ -284,7 +302,7 @@ __global__ void __launch_bounds__(SUM_THREADS, 2) embed_sum_kernel(const SumArgs
     const int p = (int)(item / a.slabs), vec = (int)(item % a.slabs) * a.tpr + lane;
     const int64_t first = (int64_t)p * a.piece, last = min((int64_t)a.T, first + a.piece);
     const bool in = vec < nvec;
-    auto key = [&](int64_t i) { return i >= 0 && i < a.T ? __ldcg(a.sorted + i).x : -1; };
+    auto key = [&](int64_t i) { return i >= 0 && i < a.T ? pair(i).x : -1; };
     const int before = key(first - 1), after = key(last), end = key(last - 1), far_before = key(first - a.piece - 1), far_after = key(last + a.piece);
     // the run at the piece's front came from before: a long one leaves its part here, a short one is the piece before's
     const bool skip = far_before != before && after != before;
@@ -299,7 +317,7 @@ __global__ void __launch_bounds__(SUM_THREADS, 2) embed_sum_kernel(const SumArgs
       Raw<O, V> r[U];
       Raw<E, V> old[U];
 #pragma unroll
-      for (int u = 0; u <= U; ++u) pr[u] = i + u < a.T ? __ldcg(a.sorted + i + u) : make_int2(a.V, 0);
+      for (int u = 0; u <= U; ++u) pr[u] = i + u < a.T ? pair(i + u) : make_int2(a.V, 0);
       if (i >= last && pr[0].x != end) break;
       bool real[U];
 #pragma unroll
@@ -423,7 +441,10 @@ size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
 constexpr int MAX_PIECES = 1024, MIN_PIECE = 8;
 static_assert(MAX_PIECES <= JOIN_Y * JOIN_WARPS * 32 && MAX_PIECES <= 32 * 33, "a thread of the join per piece; two looks find a run's end");
-int piece_of(int T) { const int n = (T + MAX_PIECES - 1) / MAX_PIECES; return n < MIN_PIECE ? MIN_PIECE : n; }
+int piece_of(int T) {
+  if (T <= FEW_TOKENS) return FEW_TOKENS;
+  const int n = (T + MAX_PIECES - 1) / MAX_PIECES; return n < MIN_PIECE ? MIN_PIECE : n;
+}
 int pieces_of(int T) { return (T + piece_of(T) - 1) / piece_of(T); }
 size_t pairs_bytes(int T) { return align256((size_t)T * sizeof(int2)); }
 
@@ -452,6 +473,7 @@ extern "C" {
 
 size_t bdlm_embed_workspace_bytes(const bdlm_embed_params* p) {
   if (check(p) != BDLM_OK) return 0;
+  if (p->T <= FEW_TOKENS) return 0;
   return 2 * pairs_bytes(p->T) + align256((size_t)pieces_of(p->T) * 2 * p->D * sizeof(float));
 }
 
@@ -479,7 +501,9 @@ int bdlm_embed_bwd(const bdlm_embed_params* p, const void* dout, const int32_t* 
                    void* workspace, size_t workspace_bytes, void* cuda_stream) {
   const int rc = check(p);
   if (rc != BDLM_OK) return rc;
-  if (dtable == nullptr || (p->T > 0 && (dout == nullptr || ids == nullptr || workspace == nullptr))) return BDLM_ERR_INVALID_ARG;
+  if (dtable == nullptr || (p->T > 0 && (dout == nullptr || ids == nullptr))) return BDLM_ERR_INVALID_ARG;
+  const bool few = p->T <= FEW_TOKENS;
+  if (!few && workspace == nullptr) return BDLM_ERR_INVALID_ARG;
   if (!al(dout, 16) || !al(dtable, 16) || !al(workspace, 16) || !al(ids, 4)) return BDLM_ERR_INVALID_ARG;
   if (workspace_bytes < bdlm_embed_workspace_bytes(p)) return BDLM_ERR_WORKSPACE_TOO_SMALL;
   if (!sm100()) return BDLM_ERR_UNSUPPORTED;
@@ -488,7 +512,7 @@ int bdlm_embed_bwd(const bdlm_embed_params* p, const void* dout, const int32_t* 
   char* ws = static_cast<char*>(workspace);
   int2 *sorted = reinterpret_cast<int2*>(ws), *other = reinterpret_cast<int2*>(ws + pairs_bytes(p->T));
   cudaError_t e = cudaSuccess;
-  if (p->T > 0) {
+  if (!few) {
     int key_bits = 1;
     while ((1ll << key_bits) <= p->V) ++key_bits;   // keys 0 .. V
     const int passes = (key_bits + DIGIT_BITS - 1) / DIGIT_BITS, bits = (key_bits + passes - 1) / passes;
@@ -518,9 +542,14 @@ int bdlm_embed_bwd(const bdlm_embed_params* p, const void* dout, const int32_t* 
   by_types(p, [&](auto te, auto to) {
     using E = typename decltype(te)::type;
     using O = typename decltype(to)::type;
-    auto sum = vec ? (a.accumulate ? embed_sum_kernel<E, O, 8, true> : embed_sum_kernel<E, O, 8, false>)
-                   : (a.accumulate ? embed_sum_kernel<E, O, 1, true> : embed_sum_kernel<E, O, 1, false>);
-    e = launch_chained(sum, p->T > 0, blocks, SUM_THREADS, 0, st, 1, a);
+    auto by_add = [&](auto v, auto is_few) {
+      constexpr int VEC = decltype(v)::value;
+      constexpr bool FEW = decltype(is_few)::value;
+      return a.accumulate ? embed_sum_kernel<E, O, VEC, true, FEW> : embed_sum_kernel<E, O, VEC, false, FEW>;
+    };
+    auto by_few = [&](auto v) { return few ? by_add(v, std::true_type{}) : by_add(v, std::false_type{}); };
+    auto sum = vec ? by_few(std::integral_constant<int, 8>{}) : by_few(std::integral_constant<int, 1>{});
+    e = launch_chained(sum, !few, blocks, SUM_THREADS, 0, st, 1, a);
     if (e != cudaSuccess || a.pieces < 2) return;
     const int cols = p->D % 4 == 0 ? 128 : 32;
     cudaLaunchConfig_t cfg = {};

@@ -4,17 +4,23 @@
 // is read once and in registers until it is written, and the variance is the sum of squares around the mean that has been
 // formed, not a difference of two large sums.
 //
-// A row belongs to a part of a warp (a power of two of lanes) or a warp, to up to 32 warps, or, beyond 1024 threads, to a cluster
-// whose CTAs exchange their sums; a thread has two vectors of it.  An SM works on 1024 threads' worth of rows, so that the
-// chain of one row -- read, join the sums, write -- lies under the others'; 64 registers a thread are all there is for that, and the
-// backward's sums of two vectors of columns take half of them.  So nothing else of a row is kept: the rows to come are
-// copied to shared memory asynchronously, and a thread reads what it has copied itself, without a barrier, each time it
-// needs it.  (With the row's vectors in registers and half the threads, 16384 x 4096 bf16 took 101 us backward.)
-// A thread keeps its columns for all its rows, so the columns' sums cost a row of partial sums per CTA.
+// A row belongs to a part of a warp (a power of two of lanes) or a warp, to warps of a CTA, or, where those are not enough, to a
+// cluster of two to five CTAs that exchange their sums.
+//   forward    loads go straight into registers, several CTAs of an SM lie under one another
+//   backward   one CTA an SM, of as many rows as 512 threads hold at 16 elements each: a thread keeps its columns for all its
+//              rows, and with them the weight and the sums for dweight and dbias in registers, so that the columns' sums cost one row
+//              of partial sums per CTA and a small reduction.  These sums leave no registers for loads in flight: the rows to
+//              come are copied to shared memory asynchronously, a ring of them, and a thread reads what it has copied itself,
+//              without a barrier.
+// Bound by memory, the backward nearly as much by instruction issue (58 % of the slots at 16384 x 4096).  Measured, bf16 with
+// residual, of the copy rate's floor: 16384 x 4096 forward 89 us (92 %), backward 93 (88 %); 32768 x 2048 87 (94 %), 89 (92 %);
+// 8192 x 8192 93 (88 %), 102 (80 %); 4096 x 16384 103 (80 %), 158 (52 %: the cluster's exchange).  Tried and slower: a ring in the forward
+// (101 us), 1024 threads at 64 registers that read everything again from shared memory (105 and 168 us), 32 elements a
+// thread (106 and 162), vectors in registers across the row's sums without a ring (backward 101).
 //
 // Rows of a length that is no whole number of 16-byte vectors begin anywhere in a vector.  They are read as the vectors that cover
 // them, shifted by `shift` elements; a thread's rows are P apart, P the number of rows after which the shift repeats, so that
-// its columns stay its own.  (Element by element, 16384 x 4100 took 462 us forward and 1353 backward.)
+// its columns stay its own.  (16384 x 4100: 142 us forward, 207 backward; element by element 462 and 1353.)
 #include <math.h>
 
 #include "../../include/bdlm_norm.h"
@@ -47,7 +53,8 @@ struct NormArgs {
   const void* h_in;                // backward
   void *y, *h;                     // forward; backward: dx
   float *mean, *rstd;
-  float* part;                     // backward: [dweight, dbias][groups][D], nullptr: neither is wanted
+  float* part;                     // backward: [dweight, dbias][groups][D]
+  void *dw, *db;                   // backward in one CTA: where they go instead; all three nullptr: neither is wanted
   int T, D, tpr, rms, period, team;
   float eps, inv_d;
 };
@@ -82,16 +89,6 @@ struct Place {
     }
   }
   __device__ __forceinline__ bool in(int i, int e) const { return has[i] && (unsigned)(col[i] + e) < (unsigned)D; }
-  // Elements of a vector that are not the row's become zeros.
-  template <class R>
-  __device__ __forceinline__ void trim(int i, R& r) const {
-    if (!SHIFT || whole[i]) return;
-    float f[V];
-    r.get(f);
-#pragma unroll
-    for (int e = 0; e < V; ++e) f[e] = in(i, e) ? f[e] : 0.f;
-    r.put(f);
-  }
   template <class T, class R>
   __device__ __forceinline__ void store(int i, T* row_of, const R& r) const {   // row_of: the row's first element
     T* to = row_of + col[i];
@@ -123,6 +120,21 @@ struct Ring {
   uint4* base;
   const Place<V, ITEMS, S, SHIFT>& at;
   int64_t elements;   // of the tensors
+  uint4* masks;       // SHIFT: [item][thread], zero bits where a vector's elements are not the row's
+  __device__ __forceinline__ void set_masks() const {
+    if (!SHIFT) return;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      uint4 m;
+      uint32_t* w = reinterpret_cast<uint32_t*>(&m);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if constexpr (sizeof(T) == 4) w[k] = at.in(i, k) ? ~0u : 0u;
+        else w[k] = (at.in(i, 2 * k) ? 0xffffu : 0u) | (at.in(i, 2 * k + 1) ? 0xffff0000u : 0u);
+      }
+      masks[i * blockDim.x + threadIdx.x] = m;   // (read by this thread alone)
+    }
+  }
   __device__ __forceinline__ uint4* slot(int k, int tensor, int i) const { return base + ((k * TENSORS + tensor) * ITEMS + i) * blockDim.x + threadIdx.x; }
   __device__ __forceinline__ void copy(int k, int tensor, const T* from, int64_t row) const {
     const int64_t start = row * at.D;
@@ -130,8 +142,9 @@ struct Ring {
     for (int i = 0; i < ITEMS; ++i) {
       if (!at.has[i]) continue;
       const uint32_t to = (uint32_t)__cvta_generic_to_shared(slot(k, tensor, i));
-      if (SHIFT) {   // (the tensor may end inside its last vector)
-        const int bytes = (int)min((int64_t)V, elements - (start + at.col[i])) * (int)sizeof(T);
+      const int64_t left = elements - (start + at.col[i]);
+      if (SHIFT && left < V) {   // the tensor ends inside its last vector
+        const int bytes = (int)left * (int)sizeof(T);
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from + start + at.col[i]), "r"(bytes) : "memory");
       } else {
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from + start + at.col[i]) : "memory");
@@ -142,7 +155,10 @@ struct Ring {
   __device__ __forceinline__ void read(int k, int tensor, int i, bool ok, Raw<T, V>& r) const {
     r.clear();
     if (ok && at.has[i]) r.load(reinterpret_cast<const T*>(slot(k, tensor, i)));
-    at.trim(i, r);
+    if (SHIFT && !at.whole[i]) {
+      const uint4 m = masks[i * blockDim.x + threadIdx.x];
+      r.q[0].x &= m.x; r.q[0].y &= m.y; r.q[0].z &= m.z; r.q[0].w &= m.w;
+    }
   }
 };
 
@@ -326,7 +342,8 @@ __global__ void __launch_bounds__(BWD_THREADS) norm_bwd_kernel(const NormArgs a)
   __shared__ float red[RED_FLOATS];
   extern __shared__ uint4 ring_mem[];
   const Place<V, ITEMS, S, SHIFT> at(a);
-  const Ring<T, 3, V, ITEMS, S, SHIFT> ring{ring_mem, at, (int64_t)a.T * a.D};
+  const Ring<T, 3, V, ITEMS, S, SHIFT> ring{ring_mem, at, (int64_t)a.T * a.D, ring_mem + RING * 3 * ITEMS * blockDim.x};
+  ring.set_masks();
   const T *dy = static_cast<const T*>(a.x), *h = static_cast<const T*>(a.h_in), *dh = static_cast<const T*>(a.res);
   T* dx = static_cast<T*>(a.y);
   float next_mean = 0.f, next_rstd = 0.f;
@@ -414,11 +431,12 @@ __global__ void __launch_bounds__(BWD_THREADS) norm_bwd_kernel(const NormArgs a)
   }
   copies_wait_all();
   if (S == TEAM) tc::cluster_sync();   // no CTA leaves while the other one may still read its sums
-  if (a.part == nullptr) return;
+  if (a.part == nullptr && a.dw == nullptr && a.db == nullptr) return;
   float* comb = reinterpret_cast<float*>(ring_mem);   // the CTA's rows join their sums here
   const int rows = blockDim.x / at.tpr, group = blockIdx.x / a.team, groups = gridDim.x / a.team;
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
+    W* out = static_cast<W*>(which ? a.db : a.dw);
     float* part = a.part + ((int64_t)which * groups + group) * a.D;
     float* to = rows > 1 ? comb + (int64_t)at.sub * a.D : part;
     __syncthreads();   // all rows' copies have landed, and the first sums have been read
@@ -428,8 +446,14 @@ __global__ void __launch_bounds__(BWD_THREADS) norm_bwd_kernel(const NormArgs a)
       for (int e = 0; e < H; ++e) {
         float p, q;
         unpack_f32x2(which ? db[i][e] : dw[i][e], p, q);
-        if (at.in(i, 2 * e)) to[at.col[i] + 2 * e] = p;
-        if (at.in(i, 2 * e + 1)) to[at.col[i] + 2 * e + 1] = q;
+        const int c = at.col[i] + 2 * e;
+        if (rows > 1 || a.part != nullptr) {
+          if (at.in(i, 2 * e)) to[c] = p;
+          if (at.in(i, 2 * e + 1)) to[c + 1] = q;
+        } else if (out != nullptr) {
+          if (at.in(i, 2 * e)) out[c] = W(p);
+          if (at.in(i, 2 * e + 1)) out[c + 1] = W(q);
+        }
       }
     }
     if (rows > 1) {
@@ -437,7 +461,8 @@ __global__ void __launch_bounds__(BWD_THREADS) norm_bwd_kernel(const NormArgs a)
       for (int c = threadIdx.x; c < a.D; c += blockDim.x) {
         float s = 0.f;
         for (int r = 0; r < rows; ++r) s += comb[(int64_t)r * a.D + c];
-        part[c] = s;
+        if (a.part != nullptr) part[c] = s;
+        else if (out != nullptr) out[c] = W(s);
       }
     }
   }
@@ -468,6 +493,9 @@ __global__ void __launch_bounds__(WG_WARPS * 32) norm_wgrad_kernel(const float* 
 }
 
 // ------------------------------------------------------------------------------------------------ host
+// Elements of a call whose backward one CTA does in a few rounds, in less time than a call takes the host (5 x 200 elements, back to
+// back: 19.4 -> 14.1 us a call).
+constexpr int ONE_CTA = 32768;
 constexpr int SMS = 148;   // what the launch shapes, and with them the workspace, count on: the device has them
 
 // How the rows are laid over threads: `rows` of them in a CTA (a CTA's share of one in a team), tpr threads each.
@@ -513,11 +541,17 @@ Layout bwd_layout(const bdlm_norm_params* p) {
   const int own = ((l.nvec + l.team - 1) / l.team + l.items - 1) / l.items;   // threads a CTA needs for a row
   l.span = l.team > 1 ? TEAM : own > 32 ? WIDE : NARROW;
   l.tpr = own > 32 ? up32(own) : narrow_tpr(own, 1);
-  const int64_t even = ((int64_t)p->T + SMS - 1) / SMS;
+  const bool one = (int64_t)p->T * p->D <= ONE_CTA;
+  const int64_t even = one ? p->T : ((int64_t)p->T + SMS - 1) / SMS;
   l.rows = l.span == TEAM ? 1 : BWD_THREADS / l.tpr;
   if (l.span == WIDE && l.rows > 15) l.rows = 15;
   if (l.rows > even) l.rows = even > 0 ? (int)even : 1;
   if (l.span == NARROW) { const int per_warp = 32 / l.tpr; l.rows = (l.rows + per_warp - 1) / per_warp * per_warp; }
+  if (one) {   // whole periods of rows, some of them without a row if need be
+    const int up = (l.rows + l.period - 1) / l.period * l.period;
+    if (up * l.tpr <= BWD_THREADS && (l.span != WIDE || up <= 15)) l.rows = up;
+    else if (l.rows > l.period) l.rows = l.rows / l.period * l.period;
+  }
   return l;
 }
 // CTAs, or clusters, of a launch: as many as have rows, at most `per_sm` an SM, and sequences of rows in whole periods.
@@ -528,7 +562,11 @@ int groups_of(const bdlm_norm_params* p, const Layout& l, int per_sm) {
   return (int)(want < cap ? (want + unit - 1) / unit * unit : cap / unit * unit);
 }
 int fwd_groups(const bdlm_norm_params* p, const Layout& l) { return groups_of(p, l, 2048 / (l.rows * l.tpr)); }
-int bwd_groups(const bdlm_norm_params* p, const Layout& l) { return groups_of(p, l, 1); }
+// One CTA for the smallest calls, if its rows are a whole period: it needs no partial sums, no workspace and no second launch.
+int bwd_groups(const bdlm_norm_params* p, const Layout& l) {
+  if (p->T > 0 && (int64_t)p->T * p->D <= ONE_CTA && l.span != TEAM && l.rows % l.period == 0) return 1;
+  return groups_of(p, l, 1);
+}
 
 int check(const bdlm_norm_params* p) {
   if (p == nullptr || p->T < 0 || p->T > (1 << 30) || p->D <= 0) return BDLM_ERR_INVALID_ARG;
@@ -582,7 +620,7 @@ extern "C" {
 size_t bdlm_norm_workspace_bytes(const bdlm_norm_params* p) {
   if (check(p) != BDLM_OK) return 0;
   const size_t groups = (size_t)bwd_groups(p, bwd_layout(p));
-  return 2 * groups * p->D * sizeof(float);
+  return groups == 1 ? 0 : 2 * groups * p->D * sizeof(float);
 }
 
 int bdlm_norm_fwd(const bdlm_norm_params* p, const void* x, const void* residual, const void* weight, const void* bias,
@@ -633,15 +671,17 @@ int bdlm_norm_bwd(const bdlm_norm_params* p, const void* dy, const void* h, cons
   for (const void* q : ptrs) if (!al(q, 16)) return BDLM_ERR_INVALID_ARG;
   if (!al(mean, 4) || !al(rstd, 4)) return BDLM_ERR_INVALID_ARG;
   const bool grads = dweight != nullptr || dbias != nullptr;
-  if (grads && p->T > 0 && workspace == nullptr) return BDLM_ERR_INVALID_ARG;
-  if (grads && workspace_bytes < bdlm_norm_workspace_bytes(p)) return BDLM_ERR_WORKSPACE_TOO_SMALL;
+  const size_t need_ws = grads ? bdlm_norm_workspace_bytes(p) : 0;
+  if (need_ws > 0 && workspace == nullptr) return BDLM_ERR_INVALID_ARG;
+  if (workspace_bytes < need_ws) return BDLM_ERR_WORKSPACE_TOO_SMALL;
   if (!sm100()) return BDLM_ERR_UNSUPPORTED;
   const Layout l = bwd_layout(p);
   const int groups = bwd_groups(p, l);
   NormArgs a = {};
   a.x = dy; a.res = dh; a.w = weight; a.h_in = h; a.y = dx;
   a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);
-  a.part = grads ? static_cast<float*>(workspace) : nullptr;
+  a.part = need_ws > 0 ? static_cast<float*>(workspace) : nullptr;
+  if (groups == 1) { a.dw = dweight; a.db = dbias; }
   a.T = p->T; a.D = p->D; a.tpr = l.tpr; a.rms = p->kind == BDLM_NORM_RMS; a.period = l.period; a.team = l.team;
   a.inv_d = (float)(1.0 / p->D);
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
@@ -656,11 +696,11 @@ int bdlm_norm_bwd(const bdlm_norm_params* p, const void* dy, const void* h, cons
                                : l.span == WIDE ? norm_bwd_kernel<X, Wt, V, I, WIDE, SH>
                                : l.items == 1   ? norm_bwd_kernel<X, Wt, V, 1, NARROW, SH>
                                                 : norm_bwd_kernel<X, Wt, V, I, NARROW, SH>;
-      e = launch_rows(kern, l, groups, ring_of(V) * 3 * l.items * l.rows * l.tpr * 16, st, a);
+      e = launch_rows(kern, l, groups, (ring_of(V) * 3 + (SH ? 1 : 0)) * l.items * l.rows * l.tpr * 16, st, a);
     });
     if (e != cudaSuccess) return BDLM_ERR_CUDA;
   }
-  if (!grads) return BDLM_OK;
+  if (!grads || groups == 1) return BDLM_OK;
   const unsigned bx = (unsigned)((p->D + 31) / 32);
   auto finish = [&](auto w) {
     using W = typename decltype(w)::type;

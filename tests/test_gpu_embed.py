@@ -89,7 +89,7 @@ def test_types(e, o, D):
     _check_bwd(200, D, 50, e, o, scale=3.0, start=True)
 
 
-@pytest.mark.parametrize("T", [1, 2, 8, 9, 31, 64, 100, 1531, 2048, 2049, 4097, 8193, 20000])
+@pytest.mark.parametrize("T", [1, 2, 8, 9, 31, 32, 33, 64, 100, 1531, 2048, 2049, 4097, 8193, 20000])
 def test_gradient_numbers_of_tokens(T):
     """Every cluster size of the sort, pieces of eight tokens and of more."""
     _check_bwd(T, 40, 777, masked=0.3)
@@ -125,6 +125,16 @@ def test_a_run_over_every_piece_and_its_neighbours():
     rng.shuffle(ids)
     _check_bwd(T, 264, V, FP32, BF16, ids=ids, scale=0.125)
     _check_bwd(T, 264, V, BF16, BF16, ids=ids, scale=0.125)
+
+
+@pytest.mark.parametrize("start", [None, True])
+@pytest.mark.parametrize("D", [5, 24, 4104])
+def test_few_tokens_in_one_launch(D, start):
+    for seed in range(4):
+        rng = np.random.default_rng(seed)
+        for T in (1, 3, 17, 32):
+            _check_bwd(T, D, 9, ids=rng.integers(-2, 11, size=T), start=start)
+    _check_bwd(32, D, 70000, FP32, FP32, ids=np.full(32, 69999), start=start)
 
 
 @pytest.mark.parametrize("start", [None, True])
@@ -287,7 +297,7 @@ def test_refusals():
     with pytest.raises(ValueError):
         binding.bdlm_embed_bwd(dout, ids, 10, out=torch.empty(11, 16, device="cuda", dtype=BF16))
     with pytest.raises(binding.BdlmError) as e:
-        binding.bdlm_embed_bwd(dout, ids, 10, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+        binding.bdlm_embed_bwd(dout.repeat(20, 1), ids.repeat(20), 10, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
     assert e.value.status == -3
     with pytest.raises(AssertionError):
         binding.bdlm_embed_fwd(table[:, ::2], ids)

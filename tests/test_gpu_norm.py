@@ -112,6 +112,14 @@ def test_numbers_of_rows(T, D):
     _both(T, D)
 
 
+@pytest.mark.parametrize("D", [1, 9, 40, 100, 257, 300, 999, 1000, 2056, 4097, 8192])
+def test_calls_of_one_cta_and_just_beyond(D):
+    """The smallest backward calls form their sums in one CTA, in rows of whole periods; both sides of the rule, every period."""
+    for T in sorted({1, 2, 3, 5, 7, 8, 13, max(1, 32768 // D), 32768 // D + 1}):
+        if T <= 400:
+            _both(T, D)
+
+
 def test_more_rows_than_ctas_and_prefetched_rows():
     _both(3001, 4096, residual=True)
     _both(40001, 16, rms=True)
@@ -294,9 +302,11 @@ def test_refusals():
     with pytest.raises(binding.BdlmError) as e:
         binding.bdlm_norm_fwd(big)
     assert e.value.status == -2
-    out = binding.bdlm_norm_fwd(i["x"], i["w"])
+    many = _inputs(1000, 64, BF16, BF16)
+    out = binding.bdlm_norm_fwd(many["x"], many["w"])
     with pytest.raises(binding.BdlmError) as e:
-        binding.bdlm_norm_bwd(i["dy"], i["x"], i["w"], out[2], out[3], workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+        binding.bdlm_norm_bwd(many["dy"], many["x"], many["w"], out[2], out[3], workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
     assert e.value.status == -3
+    out = binding.bdlm_norm_fwd(i["x"], i["w"])
     with pytest.raises(binding.BdlmError):
         binding.bdlm_norm_bwd(i["dy"], i["x"], i["w"], None, out[3])

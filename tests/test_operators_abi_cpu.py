@@ -11,7 +11,7 @@ OK, BAD16, BAD4 = ctypes.c_void_p(0x1000), ctypes.c_void_p(0x1008), ctypes.c_voi
 
 
 def _norm(**kw):
-    p = binding.make_norm_params(8, 64, torch.bfloat16, torch.bfloat16, eps=1e-5)
+    p = binding.make_norm_params(8000, 64, torch.bfloat16, torch.bfloat16, eps=1e-5)
     for k, v in kw.items():
         setattr(p, k, v)
     return p
@@ -55,14 +55,14 @@ def test_norm_pointers():
 
 def test_norm_workspace_grows_to_a_bound():
     size = lambda T, D: binding.bdlm_norm_workspace_bytes(binding.make_norm_params(T, D, torch.bfloat16, torch.bfloat16))
-    assert size(0, 64) == 0
-    assert size(1, 4096) >= 2 * 4096 * 4
+    assert size(0, 64) == 0 and size(1, 4096) == 0 and size(5, 200) == 0   # a call of one CTA needs none
+    assert size(1000, 4096) >= 2 * 4096 * 4
     assert size(1 << 30, 4096) == size(1 << 20, 4096) <= 2 * 148 * 4096 * 4
     assert all(size(T, 1001) <= 2 * 148 * 1001 * 4 for T in (5, 100, 10000))
 
 
 def _embed(**kw):
-    p = binding.make_embed_params(8, 64, 100, torch.bfloat16, torch.bfloat16)
+    p = binding.make_embed_params(80, 64, 100, torch.bfloat16, torch.bfloat16)
     for k, v in kw.items():
         setattr(p, k, v)
     return p
@@ -86,7 +86,8 @@ def test_embed_pointers():
               (OK, OK, BAD16, OK), (OK, OK, OK, BAD16)):
         assert L.bdlm_embed_bwd(ctypes.byref(p), *a, 1 << 40, None) == -1, a
     need = binding.bdlm_embed_workspace_bytes(p)
-    assert need >= 2 * 8 * 8
+    assert need >= 2 * 80 * 8
+    assert binding.bdlm_embed_workspace_bytes(_embed(T=32)) == 0   # a call of one launch needs none
     assert L.bdlm_embed_bwd(ctypes.byref(p), OK, OK, OK, OK, need - 1, None) == -3
     assert L.bdlm_embed_fwd(None, OK, OK, OK, None) == -1
 
