@@ -2,6 +2,8 @@
 #pragma once
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "../../include/bdlm_dtypes.h"
 #include "bdlm_common.cuh"
 
@@ -9,23 +11,25 @@ namespace bdlm {
 
 using bf16_t = __nv_bfloat16;
 
-// V elements of type T as they lie in memory: whole 16-byte vectors, or one element.
+// V elements of type T as they lie in memory: 16-byte vectors, one of 8 bytes, or one element.
 template <class T, int V>
 struct Raw {
   static constexpr int WORDS = V * (int)sizeof(T) / 4;
-  static_assert(WORDS % 4 == 0, "16-byte vectors");
-  uint4 q[WORDS / 4];
+  static_assert(WORDS % 4 == 0 || WORDS == 2, "16- or 8-byte vectors");
+  using Vec = typename std::conditional<WORDS == 2, uint2, uint4>::type;
+  static constexpr int N = WORDS * 4 / (int)sizeof(Vec);
+  Vec q[N];
   __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
-    for (int i = 0; i < WORDS / 4; ++i) q[i] = reinterpret_cast<const uint4*>(p)[i];
+    for (int i = 0; i < N; ++i) q[i] = reinterpret_cast<const Vec*>(p)[i];
   }
   __device__ __forceinline__ void store(T* p) const {
 #pragma unroll
-    for (int i = 0; i < WORDS / 4; ++i) reinterpret_cast<uint4*>(p)[i] = q[i];
+    for (int i = 0; i < N; ++i) reinterpret_cast<Vec*>(p)[i] = q[i];
   }
   __device__ __forceinline__ void clear() {
 #pragma unroll
-    for (int i = 0; i < WORDS / 4; ++i) q[i] = make_uint4(0u, 0u, 0u, 0u);
+    for (int i = 0; i < N; ++i) q[i] = Vec{};
   }
   __device__ __forceinline__ void get(float (&f)[V]) const {
     const uint32_t* w = reinterpret_cast<const uint32_t*>(q);

@@ -22,7 +22,6 @@
 namespace bdlm {
 namespace {
 
-__device__ __forceinline__ uint32_t ctas_of_cluster() { uint32_t n; asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(n)); return n; }
 __device__ __forceinline__ uint32_t cta_of_cluster() { uint32_t n; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(n)); return n; }
 // Also orders the CTAs' writes to global memory before the others' reads of it (release and acquire at cluster scope).
 __device__ __forceinline__ void whole_cluster_sync() {
@@ -37,8 +36,42 @@ __device__ __forceinline__ int ld_cluster_int(const int* own, int rank) {
 __device__ __forceinline__ void wait_for_sort() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
+// What a thread of a group of `tpr` has of a row's slab: a vector, or, where rows are no whole number of those, eight single elements
+// tpr apart.
+template <class T, int V>
+struct Slice {
+  static constexpr int C = V > 1 ? V : 8;
+  Raw<T, V> q[V > 1 ? 1 : 8];
+  __device__ __forceinline__ static int first(int slab, int tpr, int lane) { return V > 1 ? (slab * tpr + lane) * V : slab * 8 * tpr + lane; }   // its first column
+  __device__ __forceinline__ void load(const T* row, int at, int tpr, int D) {
+    if (V > 1) { q[0].load(row + at); return; }
+#pragma unroll
+    for (int e = 0; e < C / (V > 1 ? V : 1); ++e) {
+      const int c = at + e * tpr;
+      q[e].clear();
+      if (c < D) q[e].load(row + c);
+    }
+  }
+  __device__ __forceinline__ void store(T* row, int at, int tpr, int D) const {
+    if (V > 1) { q[0].store(row + at); return; }
+#pragma unroll
+    for (int e = 0; e < C / (V > 1 ? V : 1); ++e) {
+      const int c = at + e * tpr;
+      if (c < D) q[e].store(row + c);
+    }
+  }
+  __device__ __forceinline__ void get(float (&f)[C]) const {
+#pragma unroll
+    for (int e = 0; e < C / V; ++e) q[e].get(reinterpret_cast<float (&)[V]>(f[e * V]));
+  }
+  __device__ __forceinline__ void put(const float (&f)[C]) {
+#pragma unroll
+    for (int e = 0; e < C / V; ++e) q[e].put(reinterpret_cast<const float (&)[V]>(f[e * V]));
+  }
+};
+
 // ------------------------------------------------------------------------------------------------ lookup
-// `tpr` threads (a power of two) share a row, four vectors of it in flight in each.
+// `tpr` threads (a power of two) share a row, four vectors or eight elements of it in flight in each.
 template <class E, class O, int V>
 __global__ void __launch_bounds__(256) embed_fwd_kernel(const E* table, const int* ids, O* out, int T, int D, int vocab, int tpr, float scale) {
   const int rows = 256 / tpr, lane = threadIdx.x % tpr;
@@ -49,7 +82,7 @@ __global__ void __launch_bounds__(256) embed_fwd_kernel(const E* table, const in
   const int nvec = D / V;
   const E* src = table + (int64_t)(real ? id : 0) * D;
   O* dst = out + row * D;
-  constexpr int U = 4;
+  constexpr int U = V > 1 ? 4 : 8;
   for (int c0 = lane; c0 < nvec; c0 += U * tpr) {
     Raw<E, V> r[U];
 #pragma unroll
@@ -88,8 +121,8 @@ __global__ void __launch_bounds__(SORT_WARPS * 32) embed_sort_kernel(const int* 
   int* scan = base + BINS;
   let_next_start();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, bins = 1 << bits;
-  const int ctas = (int)ctas_of_cluster(), rank = (int)cta_of_cluster();
-  const int warps = ctas * SORT_WARPS;
+  const int rank = (int)cta_of_cluster();
+  constexpr int warps = SORT_CTAS * SORT_WARPS;
   const int64_t seg = (((int64_t)T + warps - 1) / warps + 31) / 32 * 32;
   const int64_t first = min((int64_t)T, (int64_t)(rank * SORT_WARPS + warp) * seg), last = min((int64_t)T, first + seg);
   int* mine = hist + warp * BINS;
@@ -112,7 +145,7 @@ __global__ void __launch_bounds__(SORT_WARPS * 32) embed_sort_kernel(const int* 
       for (int k = 0; k < HELD; ++k) held[k] = pair_at(i + 32 * k + lane);
     };
     if (few) request(first);
-    for (int b = threadIdx.x; b < SORT_WARPS * BINS; b += SORT_WARPS * 32) hist[b] = 0;
+    for (int b = threadIdx.x; b < SORT_WARPS * BINS / 4; b += SORT_WARPS * 32) reinterpret_cast<int4*>(hist)[b] = make_int4(0, 0, 0, 0);
     __syncthreads();
     for (int64_t i = first; i < last; i += 32 * HELD) {
       if (!few) request(i);
@@ -140,11 +173,11 @@ __global__ void __launch_bounds__(SORT_WARPS * 32) embed_sort_kernel(const int* 
     // exclusive sums over the bins of all CTAs, and the lower CTAs' pairs of the same bin
     int all = 0, lower = 0;
     if ((int)threadIdx.x < bins) {
-      for (int c = 0; c < ctas; ++c) {
-        const int n = ld_cluster_int(total + threadIdx.x, c);
-        all += n;
-        if (c < rank) lower += n;
-      }
+      int n[SORT_CTAS];   // all on their way at once
+#pragma unroll
+      for (int c = 0; c < SORT_CTAS; ++c) n[c] = ld_cluster_int(total + threadIdx.x, c);
+#pragma unroll
+      for (int c = 0; c < SORT_CTAS; ++c) { all += n[c]; lower += c < rank ? n[c] : 0; }
     }
     int up = all;
 #pragma unroll
@@ -246,14 +279,25 @@ struct SumArgs {
 constexpr int SUM_THREADS = 512, GROUP_THREADS = 128;   // threads of a CTA; of a piece's slab, at most
 constexpr int FILL_WORDS = 4096;                        // rows a CTA looks up at a time: a bit each
 
-// E: table, O: tokens' rows.  A group of `tpr` threads takes a piece and a slab of tpr V columns.
+// A warp zeros a row, wherever it begins: whole 16-byte vectors, and elements before and after them.
+template <class E>
+__device__ __forceinline__ void zero_row(E* row, int D) {
+  constexpr int PER = 16 / (int)sizeof(E);
+  const int lane = threadIdx.x & 31, head = min(D, (int)((16u - ((uintptr_t)row & 15u)) & 15u) / (int)sizeof(E));
+  const int vecs = (D - head) / PER, tail = head + vecs * PER;
+  if (lane < head) row[lane] = E(0.f);
+  uint4* at = reinterpret_cast<uint4*>(row + head);
+  for (int c = lane; c < vecs; c += 32) at[c] = make_uint4(0u, 0u, 0u, 0u);
+  if (tail + lane < D) row[tail + lane] = E(0.f);
+}
+
+// E: table, O: tokens' rows.  A group of `tpr` threads takes a piece and a slab of columns, a Slice of it each.
 // FEW: no more than FEW_TOKENS of them, one piece: each CTA sorts them itself, and this is the only launch.
 constexpr int FEW_TOKENS = 32;
 template <class E, class O, int V, bool ADD, bool FEW>
 __global__ void __launch_bounds__(SUM_THREADS, 2) embed_sum_kernel(const SumArgs a) {
   __shared__ uint32_t present[FILL_WORDS];
   E* dtable = static_cast<E*>(a.dtable);
-  const int nvec = a.D / V;
   if (!ADD) {
     const int64_t share = ((int64_t)a.V + gridDim.x - 1) / gridDim.x;
     const int64_t begin = min((int64_t)a.V, blockIdx.x * share), end = min((int64_t)a.V, begin + share);
@@ -267,13 +311,8 @@ __global__ void __launch_bounds__(SUM_THREADS, 2) embed_sum_kernel(const SumArgs
         if (at >= 0 && at < n) atomicOr(&present[at >> 5], 1u << (at & 31));
       }
       __syncthreads();
-      Raw<E, V> zero;
-      zero.clear();
-      for (int r = threadIdx.x >> 5; r < n; r += SUM_THREADS / 32) {
-        if ((present[r >> 5] >> (r & 31)) & 1u) continue;
-        E* row = dtable + (v0 + r) * a.D;
-        for (int c = threadIdx.x & 31; c < nvec; c += 32) zero.store(row + (int64_t)c * V);
-      }
+      for (int r = threadIdx.x >> 5; r < n; r += SUM_THREADS / 32)
+        if (!((present[r >> 5] >> (r & 31)) & 1u)) zero_row(dtable + (v0 + r) * a.D, a.D);
       __syncthreads();
     }
   }
@@ -299,23 +338,26 @@ __global__ void __launch_bounds__(SUM_THREADS, 2) embed_sum_kernel(const SumArgs
   const int groups = SUM_THREADS / a.tpr, lane = threadIdx.x % a.tpr;
   const int64_t items = (int64_t)a.pieces * a.slabs;
   for (int64_t item = (int64_t)blockIdx.x * groups + threadIdx.x / a.tpr; item < items; item += (int64_t)gridDim.x * groups) {
-    const int p = (int)(item / a.slabs), vec = (int)(item % a.slabs) * a.tpr + lane;
+    using Row = Slice<O, V>;
+    using Out = Slice<E, V>;
+    constexpr int N = Row::C;
+    const int p = (int)(item / a.slabs), col = Row::first((int)(item % a.slabs), a.tpr, lane);
     const int64_t first = (int64_t)p * a.piece, last = min((int64_t)a.T, first + a.piece);
-    const bool in = vec < nvec;
+    const bool in = col < a.D;
     auto key = [&](int64_t i) { return i >= 0 && i < a.T ? pair(i).x : -1; };
     const int before = key(first - 1), after = key(last), end = key(last - 1), far_before = key(first - a.piece - 1), far_after = key(last + a.piece);
     // the run at the piece's front came from before: a long one leaves its part here, a short one is the piece before's
     const bool skip = far_before != before && after != before;
     // and the run at its end goes on: a short one that begins here is followed to its end
     const bool follow = end == after && end != before && far_after != end;
-    float acc[V];
+    float acc[N];
     int run = -1;
-    constexpr int U = sizeof(E) == 4 && V > 1 && (ADD || sizeof(O) == 4) ? 2 : 4;   // tokens in flight
+    constexpr int U = V == 1 || ADD ? 2 : 4;   // tokens in flight: what 64 registers hold
     const int64_t most = follow ? min((int64_t)a.T, last + a.piece) : last;
     for (int64_t i = first; i < most; i += U) {
       int2 pr[U + 1];
-      Raw<O, V> r[U];
-      Raw<E, V> old[U];
+      Row r[U];
+      Out old[U];
 #pragma unroll
       for (int u = 0; u <= U; ++u) pr[u] = i + u < a.T ? pair(i + u) : make_int2(a.V, 0);
       if (i >= last && pr[0].x != end) break;
@@ -324,35 +366,37 @@ __global__ void __launch_bounds__(SUM_THREADS, 2) embed_sum_kernel(const SumArgs
       for (int u = 0; u < U; ++u) {
         // (padding stands last)
         real[u] = in && pr[u].x < a.V && (i + u < last ? !(skip && pr[u].x == before) : i + u < most && pr[u].x == end);
-        r[u].clear();
-        if (real[u]) r[u].load(dout + (int64_t)pr[u].y * a.D + (int64_t)vec * V);
+        if (real[u]) r[u].load(dout + (int64_t)pr[u].y * a.D, col, a.tpr, a.D);
         // what the sum is added to, where the run ends here as a whole: requested with the rows, not after them
         if (ADD && real[u] && pr[u + 1].x != pr[u].x && pr[u].x != before)
-          old[u].load(dtable + (int64_t)pr[u].x * a.D + (int64_t)vec * V);
+          old[u].load(dtable + (int64_t)pr[u].x * a.D, col, a.tpr, a.D);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         if (!real[u]) continue;
-        float f[V];
+        float f[N];
         r[u].get(f);
         const bool begins = pr[u].x != run;
         run = pr[u].x;
 #pragma unroll
-        for (int e = 0; e < V; ++e) acc[e] = begins ? f[e] : acc[e] + f[e];
+        for (int e = 0; e < N; ++e) acc[e] = begins ? f[e] : acc[e] + f[e];
         const bool goes_on = pr[u + 1].x == run, came = run == before;
         if (goes_on && (follow || i + u + 1 != last)) continue;
         if (came || goes_on) {
-          float* at = a.parts + ((int64_t)p * 2 + (came ? 0 : 1)) * a.D + (int64_t)vec * V;
+          float* at = a.parts + ((int64_t)p * 2 + (came ? 0 : 1)) * a.D;
 #pragma unroll
-          for (int e = 0; e < V; ++e) at[e] = acc[e];
+          for (int e = 0; e < N; ++e) {
+            const int c = V > 1 ? col + e : col + e * a.tpr;
+            if (V > 1 || c < a.D) at[c] = acc[e];
+          }
         } else {
-          float g[V];
+          float g[N];
           if (ADD) old[u].get(g);
 #pragma unroll
-          for (int e = 0; e < V; ++e) g[e] = ADD ? fmaf(acc[e], a.scale, g[e]) : acc[e] * a.scale;
-          Raw<E, V> o;
+          for (int e = 0; e < N; ++e) g[e] = ADD ? fmaf(acc[e], a.scale, g[e]) : acc[e] * a.scale;
+          Out o;
           o.put(g);
-          o.store(dtable + (int64_t)run * a.D + (int64_t)vec * V);
+          o.store(dtable + (int64_t)run * a.D, col, a.tpr, a.D);
         }
       }
     }
@@ -448,6 +492,13 @@ int piece_of(int T) {
 int pieces_of(int T) { return (T + piece_of(T) - 1) / piece_of(T); }
 size_t pairs_bytes(int T) { return align256((size_t)T * sizeof(int2)); }
 
+// Elements a thread takes at a time: 16 bytes of the table, where rows are whole numbers of those.  (32 bytes of an fp32 table in two
+// stores left half-written sectors: 45452 x 3224 took 174 us, now 106.)
+template <class E> constexpr int vector_of() { return 16 / (int)sizeof(E); }
+int vector_of(const bdlm_embed_params* p) {
+  const int v = p->table_dtype == BDLM_FP32 ? vector_of<float>() : vector_of<bf16_t>();
+  return p->D % v == 0 ? v : 1;
+}
 template <class T> struct Type { using type = T; };
 // Calls f(table type, row type).
 template <class F>
@@ -485,13 +536,12 @@ int bdlm_embed_fwd(const bdlm_embed_params* p, const void* table, const int32_t*
   if (!sm100()) return BDLM_ERR_UNSUPPORTED;
   if (p->T == 0) return BDLM_OK;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const bool vec = p->D % 8 == 0;
-  const int nvec = vec ? p->D / 8 : p->D, tpr = pow2_at_least((nvec + 3) / 4, 256), rows = 256 / tpr;
+  const int V = vector_of(p), nvec = p->D / V, tpr = pow2_at_least(V > 1 ? (nvec + 3) / 4 : (nvec + 7) / 8, 256), rows = 256 / tpr;
   const unsigned blocks = (unsigned)(((int64_t)p->T + rows - 1) / rows);
   by_types(p, [&](auto e, auto o) {
     using E = typename decltype(e)::type;
     using O = typename decltype(o)::type;
-    auto kern = vec ? embed_fwd_kernel<E, O, 8> : embed_fwd_kernel<E, O, 1>;
+    auto kern = V > 1 ? embed_fwd_kernel<E, O, vector_of<E>()> : embed_fwd_kernel<E, O, 1>;
     kern<<<blocks, 256, 0, st>>>(static_cast<const E*>(table), ids, static_cast<O*>(out), p->T, p->D, p->V, tpr, p->scale);
   });
   return cudaGetLastError() == cudaSuccess ? BDLM_OK : BDLM_ERR_CUDA;
@@ -526,13 +576,12 @@ int bdlm_embed_bwd(const bdlm_embed_params* p, const void* dout, const int32_t* 
     }
     if (e != cudaSuccess) return BDLM_ERR_CUDA;
   }
-  const bool vec = p->D % 8 == 0;
-  const int nvec = vec ? p->D / 8 : p->D;
+  const int V = vector_of(p), slices = V > 1 ? p->D / V : (p->D + 7) / 8;
   SumArgs a = {};
   a.dout = dout; a.ids = ids; a.sorted = sorted; a.dtable = dtable;
   a.parts = reinterpret_cast<float*>(ws + 2 * pairs_bytes(p->T));
   a.T = p->T; a.D = p->D; a.V = p->V; a.piece = piece_of(p->T); a.pieces = pieces_of(p->T);
-  a.tpr = pow2_at_least(nvec, GROUP_THREADS); a.slabs = (nvec + a.tpr - 1) / a.tpr;
+  a.tpr = pow2_at_least(slices, GROUP_THREADS); a.slabs = (slices + a.tpr - 1) / a.tpr;
   a.scale = p->scale; a.accumulate = p->accumulate;
   const int64_t items = (int64_t)a.pieces * a.slabs, groups = SUM_THREADS / a.tpr;
   int64_t want = (items + groups - 1) / groups;
@@ -548,7 +597,7 @@ int bdlm_embed_bwd(const bdlm_embed_params* p, const void* dout, const int32_t* 
       return a.accumulate ? embed_sum_kernel<E, O, VEC, true, FEW> : embed_sum_kernel<E, O, VEC, false, FEW>;
     };
     auto by_few = [&](auto v) { return few ? by_add(v, std::true_type{}) : by_add(v, std::false_type{}); };
-    auto sum = vec ? by_few(std::integral_constant<int, 8>{}) : by_few(std::integral_constant<int, 1>{});
+    auto sum = V > 1 ? by_few(std::integral_constant<int, vector_of<E>()>{}) : by_few(std::integral_constant<int, 1>{});
     e = launch_chained(sum, !few, blocks, SUM_THREADS, 0, st, 1, a);
     if (e != cudaSuccess || a.pieces < 2) return;
     const int cols = p->D % 4 == 0 ? 128 : 32;
