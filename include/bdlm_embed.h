@@ -5,7 +5,7 @@
  *     out_t = scale table[ids_t]                            rounded once
  *     dtable_v = scale sum_{t : ids_t = v} dout_t           (added to what dtable holds with accumulate = 1)
  * An id that is negative or not below V is no token (padding): its row of `out` is zero and it has no part in dtable.  The
- * gradient's sums are formed over the tokens sorted by id: in fp32, in a fixed order that depends on T only, so they are
+ * gradient's sums are formed over the tokens sorted by id: in fp32, in an order that the ids alone fix, so they are
  * bitwise reproducible however often a token occurs (the mask token of block-diffusion training is half of all noisy
  * tokens).  A training step of block-diffusion looks up clean and noisy tokens of one table: as one call over both, or as a
  * second backward with accumulate = 1, which is also how the gradient of a table that is tied to the loss head is added to

@@ -48,7 +48,7 @@ typedef struct {
   int32_t reserved[2];   /* 0 */
 } bdlm_norm_params;
 
-/* Scratch bytes of a backward that forms dweight (and dbias): fp32 partial sums of up to 148 groups of rows.  0 where
+/* Scratch bytes of a backward that forms dweight (and dbias): fp32 partial sums of groups of rows, about one a multiprocessor.  0 where
  * none are needed (the smallest calls) and for invalid parameters. */
 size_t bdlm_norm_workspace_bytes(const bdlm_norm_params* p);
 

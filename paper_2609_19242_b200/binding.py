@@ -596,7 +596,7 @@ def bdlm_norm_workspace_bytes(params: BdlmNormParams) -> int:
 def bdlm_norm_fwd(x, weight=None, bias=None, residual=None, *, eps=1e-5, rms=False, out=None):
     """Layer norm (root-mean-square norm with `rms`) of h = x + residual along the last axis: x [..., D] bf16, fp16 or fp32,
     weight and bias [D] of the same type or fp32.  Returns (y, h, mean, rstd): h is x itself where there is no residual, mean is None with
-    `rms`; mean and rstd [...] fp32 are what the backward reads.  `out` may supply those four."""
+    `rms`; mean and rstd [...] fp32 are what the backward reads.  `out` may supply those four (h: only with a residual)."""
     index, shape, dtype = _current(x), x.shape, x.dtype
     D, rows = shape[-1], shape[:-1]
     wdtype = dtype if weight is None else weight.dtype
@@ -610,6 +610,8 @@ def bdlm_norm_fwd(x, weight=None, bias=None, residual=None, *, eps=1e-5, rms=Fal
     else:
         y, h, mean, rstd = out
         y_at, h_at = _checked("y", y, shape, dtype, index), _checked("h", h, shape, dtype, index)
+        if residual is None:   # nothing is written to a buffer for h
+            out = (y, x, mean, rstd)
         mean_at, rstd_at = _checked("mean", mean, rows, torch.float32, index), _checked("rstd", rstd, rows, torch.float32, index)
     p = BdlmNormParams(x.numel() // D if D else 0, D, DTYPES[dtype], DTYPES[wdtype], NORM_RMS if rms else NORM_LAYER, eps)
     rc = lib().bdlm_norm_fwd(ctypes.byref(p), _checked("x", x, shape, dtype, index), res_at, w_at, b_at, y_at,

@@ -3,8 +3,8 @@
 // The lookup is a copy of T rows: 2 T D elements, bound by memory.
 //
 // The gradient has to read T D elements and write V D of them, most of the latter zeros (a batch holds a few thousand of
-// 128256 tokens).  Three launches, chained:
-//   sort    one cluster sorts (id, position) by id, a stable radix sort whose CTAs exchange their digits' counts through
+// 128256 tokens).  Three launches, chained (one, up to FEW_TOKENS tokens, which every CTA of the sum then sorts itself):
+//   sort    up to RANK_MOST tokens by counting: a token's place is how many come before it.  More: one cluster sorts (id, position) by id, a stable radix sort whose CTAs exchange their digits' counts through
 //           distributed shared memory; the pairs ping-pong through the workspace, which stays in L2
 //   sum     zeros the rows of tokens that do not occur -- it finds them in the ids themselves, so this runs beside the sort --
 //           and then, once the sort is done, sums the sorted tokens' rows in pieces of `piece` tokens.  A run of equal ids is
@@ -12,8 +12,8 @@
 //           piece leaves an fp32 part.  (With parts of every run that crosses a border, a third of the borders of 16384 tokens
 //           over 32008 ids had some, and joining them took 25 us of 85.)
 //   join    adds the parts of such long runs (the mask token's covers hundreds of pieces)
-// Every sum runs in the tokens' order inside a piece and over the pieces in order of sixteen interleaved shares, so it depends on
-// T only, not on how often a token occurs or where.
+// Every sum runs in the tokens' order inside a piece, and a long run's over its pieces in sixteen interleaved shares that are added in
+// order: the ids alone fix the order, and no atomics meet in a sum.
 #include <math.h>
 
 #include "../../include/bdlm_embed.h"

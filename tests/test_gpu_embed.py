@@ -2,7 +2,7 @@
 
 Tolerances.  The lookup is one fp32 product rounded once: (eps/2 + 2^-24) of the value.  A gradient row of n tokens is summed in
 fp32: at most 2 `piece` additions one after the other (piece: 8, or T / 1024), or `piece` of them and then the pieces' parts
-in eight shares, so for the sizes here it is off by at most (piece + T / (8 piece) + 16) x 2^-24 of the sum of the terms'
+in sixteen shares, so for the sizes here it is off by at most (piece + T / (8 piece) + 16) x 2^-24 of the sum of the terms'
 magnitudes (2 piece is less for T up to 147000), and rounded once."""
 import numpy as np
 import pytest

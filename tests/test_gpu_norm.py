@@ -310,3 +310,15 @@ def test_refusals():
     out = binding.bdlm_norm_fwd(i["x"], i["w"])
     with pytest.raises(binding.BdlmError):
         binding.bdlm_norm_bwd(i["dy"], i["x"], i["w"], None, out[3])
+
+
+@pytest.mark.parametrize("rms", [False, True])
+def test_supplied_outputs_without_a_residual_return_x_as_h(rms):
+    i = _inputs(5, 72, BF16, BF16)
+    want = binding.bdlm_norm_fwd(i["x"], i["w"], rms=rms)
+    buffer = torch.full_like(i["x"], 7.0)
+    stats = lambda: torch.empty(5, dtype=FP32, device="cuda")
+    got = binding.bdlm_norm_fwd(i["x"], i["w"], rms=rms, out=(torch.empty_like(i["x"]), buffer, None if rms else stats(), stats()))
+    assert got[1] is i["x"] and (buffer == 7.0).all()
+    for a, b in zip(got, want):
+        assert (a is None and b is None) or torch.equal(a, b)
