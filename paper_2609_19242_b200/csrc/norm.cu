@@ -12,15 +12,18 @@
 //              of partial sums per CTA and a small reduction.  These sums leave no registers for loads in flight: the rows to
 //              come are copied to shared memory asynchronously, a ring of them, and a thread reads what it has copied itself,
 //              without a barrier.
-// Bound by memory, the backward nearly as much by instruction issue (58 % of the slots at 16384 x 4096).  Measured, bf16 with
+// Bound by memory, the backward nearly as much by instruction issue (61 % of the slots at 8192 x 4096).  Measured, bf16 with
 // residual, of the copy rate's floor: 16384 x 4096 forward 89 us (92 %), backward 93 (88 %); 32768 x 2048 87 (94 %), 89 (92 %);
-// 8192 x 8192 93 (88 %), 102 (80 %); 4096 x 16384 103 (80 %), 158 (52 %: the cluster's exchange).  Tried and slower: a ring in the forward
-// (101 us), 1024 threads at 64 registers that read everything again from shared memory (105 and 168 us), 32 elements a
-// thread (106 and 162), vectors in registers across the row's sums without a ring (backward 101).
+// 8192 x 8192 93 (88 %), 102 (80 %); 4096 x 16384 102 (80 %), 158 (52 %: the cluster's exchange).  Without a residual the forward
+// moves half the bytes but has as many barriers and nearly as many instructions: 16384 x 4096 64 us, 64 % (57 as a root-mean-square
+// norm, which has one sum instead of two).  Tried and slower or no faster: in the forward the next row requested ahead where there is no residual
+// (68: the registers do not hold it), products packed two to an instruction (87 and 62, but 65536 x 512 51 for 46), a ring
+// (101); in both passes 1024 threads at 64 registers that read everything again from shared memory (105 and 168 us), 32 elements a
+// thread (106 and 162); in the backward vectors in registers across the row's sums without a ring (101).
 //
 // Rows of a length that is no whole number of 16-byte vectors begin anywhere in a vector.  They are read as the vectors that cover
 // them, shifted by `shift` elements; a thread's rows are P apart, P the number of rows after which the shift repeats, so that
-// its columns stay its own.  (16384 x 4100: 142 us forward, 207 backward; element by element 462 and 1353.)
+// its columns stay its own.  (16384 x 4100: 142 us forward, 206 backward; element by element 462 and 1353.)
 #include <math.h>
 
 #include "../../include/bdlm_norm.h"
@@ -37,14 +40,16 @@ using tc::pack_f32x2;
 using tc::unpack_f32x2;
 
 enum Span { NARROW, WIDE, TEAM };   // a row's threads: part of a warp or a warp; warps of a CTA; a cluster
-// Vectors of a row that a thread has.  Backward: 16 elements, or one vector of short rows.  Forward: up to four; with four and more
-// than a warp to a row, its weights are read again for each row instead of kept.
+// Vectors of a row that a thread has.  Backward: 16 elements, or one vector of short rows.  Forward: 16 elements too where a row takes
+// more than a warp, or four vectors of 32-bit elements: with four, a row's weights are read again instead of kept, which costs long
+// 16-bit rows more than the barriers of more threads do (8192 x 8191 279 us with four, 172 with two; 4096 x 16383 391,
+// 239; 6144 x 10240 122, 114).  32-bit rows lose: 2048 x 16384 90 with four, 132 with two.
 __host__ __device__ constexpr int bwd_items(int V) { return 16 / V; }
 __host__ __device__ constexpr bool fwd_long(int items, Span s) { return s != NARROW && items == 4; }
 constexpr int NARROW_THREADS = 128, BWD_THREADS = 512;   // of a CTA, at most
-__host__ __device__ constexpr int fwd_threads(int V, int items, Span s) { return s == NARROW ? NARROW_THREADS : fwd_long(items, s) && V == 4 ? 1024 : 512; }
+__host__ __device__ constexpr int fwd_threads(int V, int items, Span s) { return s == NARROW ? NARROW_THREADS : V == 4 && items == 2 ? 512 : 1024; }
 // (64 registers where a row takes a CTA: 16384 x 4095 forward 242 us with 99, 144 with these)
-__host__ __device__ constexpr int fwd_ctas(int items, Span s) { return s == WIDE && items == 2 ? 2 : s == NARROW ? (items == 4 ? 4 : 8) : 1; }
+__host__ __device__ constexpr int fwd_ctas(int V, int items, Span s) { return s == NARROW ? (items == 4 ? 4 : 8) : V == 4 && items == 2 ? 2 : 1; }
 // Rows in flight in the backward: the same number of bytes for 16- and 32-bit elements.
 __host__ __device__ constexpr int ring_of(int V) { return V == 8 ? 4 : 2; }
 
@@ -203,7 +208,7 @@ constexpr int RED_FLOATS = 2 * 32 * 2;   // two buffers in turn, 32 warps, two s
 // The forward loads a row's vectors straight into registers: a thread has nothing else to keep, so four CTAs of a 4096-element
 // row share an SM and their loads lie under one another.  (The backward's ring took 101 us here instead of 89, 16384 x 4096.)
 template <class T, class W, int V, int ITEMS, Span S, bool SHIFT>
-__global__ void __launch_bounds__(fwd_threads(V, ITEMS, S), fwd_ctas(ITEMS, S)) norm_fwd_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(fwd_threads(V, ITEMS, S), fwd_ctas(V, ITEMS, S)) norm_fwd_kernel(const NormArgs a) {
   constexpr bool LONG = fwd_long(ITEMS, S);
   __shared__ float red[RED_FLOATS];
   const int tpr = S == NARROW ? a.tpr : (int)blockDim.x, lane = S == NARROW ? (int)threadIdx.x % tpr : (int)threadIdx.x;
@@ -524,7 +529,7 @@ Layout fwd_layout(const bdlm_norm_params* p) {
     l.rows = NARROW_THREADS / l.tpr;
     return l;
   }
-  l.items = l.nvec <= 2 * fwd_threads(l.vec, 2, WIDE) ? 2 : 4;
+  l.items = l.vec == 8 || l.nvec <= 2 * fwd_threads(l.vec, 2, WIDE) ? 2 : 4;
   const int most = l.items * fwd_threads(l.vec, l.items, WIDE);
   l.team = (l.nvec + most - 1) / most;
   l.span = l.team > 1 ? TEAM : WIDE;
@@ -646,8 +651,9 @@ int bdlm_norm_fwd(const bdlm_norm_params* p, const void* x, const void* residual
     using Wt = typename decltype(w)::type;
     constexpr int V = decltype(v)::value;
     constexpr bool SH = decltype(shift)::value;
-    void (*kern)(NormArgs) = l.span == TEAM  ? norm_fwd_kernel<X, Wt, V, 4, TEAM, SH>
-                             : l.span == WIDE ? (l.items == 2 ? norm_fwd_kernel<X, Wt, V, 2, WIDE, SH> : norm_fwd_kernel<X, Wt, V, 4, WIDE, SH>)
+    constexpr int MOST = V == 8 ? 2 : 4;
+    void (*kern)(NormArgs) = l.span == TEAM  ? norm_fwd_kernel<X, Wt, V, MOST, TEAM, SH>
+                             : l.span == WIDE ? (l.items == 2 ? norm_fwd_kernel<X, Wt, V, 2, WIDE, SH> : norm_fwd_kernel<X, Wt, V, MOST, WIDE, SH>)
                              : l.items == 1   ? norm_fwd_kernel<X, Wt, V, 1, NARROW, SH>
                              : l.items == 2   ? norm_fwd_kernel<X, Wt, V, 2, NARROW, SH>
                                               : norm_fwd_kernel<X, Wt, V, 4, NARROW, SH>;
