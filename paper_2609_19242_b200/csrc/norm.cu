@@ -14,7 +14,7 @@
 //              without a barrier.
 // Bound by memory, the backward nearly as much by instruction issue (61 % of the slots at 8192 x 4096).  Measured, bf16 with
 // residual, of the copy rate's floor: 16384 x 4096 forward 89 us (92 %), backward 93 (88 %); 32768 x 2048 87 (94 %), 89 (92 %);
-// 8192 x 8192 93 (88 %), 102 (80 %); 4096 x 16384 102 (80 %), 158 (52 %: the cluster's exchange).  Without a residual the forward
+// 8192 x 8192 93 (88 %), 102 (80 %); 4096 x 16384 102 (80 %), 128 (64 %: the cluster's exchange).  Without a residual the forward
 // moves half the bytes but has as many barriers and nearly as many instructions: 16384 x 4096 64 us, 64 % (57 as a root-mean-square
 // norm, which has one sum instead of two).  Tried and slower or no faster: in the forward the next row requested ahead where there is no residual
 // (68: the registers do not hold it), products packed two to an instruction (87 and 62, but 65536 x 512 51 for 46), a ring
@@ -43,7 +43,7 @@ enum Span { NARROW, WIDE, TEAM };   // a row's threads: part of a warp or a warp
 // Vectors of a row that a thread has.  Backward: 16 elements, or one vector of short rows.  Forward: 16 elements too where a row takes
 // more than a warp, or four vectors of 32-bit elements: with four, a row's weights are read again instead of kept, which costs long
 // 16-bit rows more than the barriers of more threads do (8192 x 8191 279 us with four, 172 with two; 4096 x 16383 391,
-// 239; 6144 x 10240 122, 114).  32-bit rows lose: 2048 x 16384 90 with four, 132 with two.
+// 239, with the fences below 214; 6144 x 10240 122, 114).  32-bit rows lose: 2048 x 16384 90 with four, 132 with two.
 __host__ __device__ constexpr int bwd_items(int V) { return 16 / V; }
 __host__ __device__ constexpr bool fwd_long(int items, Span s) { return s != NARROW && items == 4; }
 constexpr int NARROW_THREADS = 128, BWD_THREADS = 512;   // of a CTA, at most
@@ -167,6 +167,14 @@ struct Ring {
   }
 };
 
+// A cluster's barrier that orders shared memory alone, which is where the sums are: a release of everything waits for the threads' stores
+// to global memory too (backward 4096 x 16384 157 us, 136 with these fences, 128 with the exchange under the next row's products as well).
+__device__ __forceinline__ void cluster_arrive() {
+  asm volatile("fence.release.sync_restrict::shared::cta.cluster;\n\tbarrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+  asm volatile("barrier.cluster.wait.acquire.aligned;\n\tfence.acquire.sync_restrict::shared::cluster.cluster;" ::: "memory");
+}
 // Sums over the threads of a row; every thread gets them.  The order is fixed, and the same in all CTAs of a cluster.
 template <Span S, int N>
 __device__ __forceinline__ void row_sum(float (&v)[N], int tpr, int sub, int team, float* red, int& turn) {
@@ -182,7 +190,7 @@ __device__ __forceinline__ void row_sum(float (&v)[N], int tpr, int sub, int tea
 #pragma unroll
     for (int n = 0; n < N; ++n) at[warp * 2 + n] = v[n];
   }
-  if (S == TEAM) tc::cluster_sync();
+  if (S == TEAM) { cluster_arrive(); cluster_wait(); }
   else asm volatile("bar.sync %0, %1;" ::"r"(sub + 1), "r"(tpr) : "memory");   // the row's warps
   at += sub * warps * 2;
 #pragma unroll
@@ -204,6 +212,33 @@ __device__ __forceinline__ void row_sum(float (&v)[N], int tpr, int sub, int tea
   }
 }
 constexpr int RED_FLOATS = 2 * 32 * 2;   // two buffers in turn, 32 warps, two sums
+// The same over a cluster in two steps: a CTA's warps put their sums down before the cluster's barrier, every warp gets all of them after it.
+__device__ __forceinline__ void team_put(float (&v)[2], float* red) {
+#pragma unroll
+  for (int s = 16; s > 0; s >>= 1) {
+    v[0] += __shfl_xor_sync(0xffffffffu, v[0], s);
+    v[1] += __shfl_xor_sync(0xffffffffu, v[1], s);
+  }
+  if ((threadIdx.x & 31) == 0) *reinterpret_cast<float2*>(red + (threadIdx.x >> 5) * 2) = make_float2(v[0], v[1]);
+}
+__device__ __forceinline__ void team_get(float (&v)[2], const float* red, int warps, int team) {
+  const int lane = threadIdx.x & 31;
+  v[0] = v[1] = 0.f;
+  if (lane < warps) {
+    const uint32_t at = tc::smem_u32(red + lane * 2);
+    for (int c = 0; c < team; ++c) {
+      float p, q;
+      asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(p), "=f"(q) : "r"(tc::peer_addr(at, c)) : "memory");
+      v[0] += p;
+      v[1] += q;
+    }
+  }
+#pragma unroll
+  for (int s = 16; s > 0; s >>= 1) {
+    v[0] += __shfl_xor_sync(0xffffffffu, v[0], s);
+    v[1] += __shfl_xor_sync(0xffffffffu, v[1], s);
+  }
+}
 
 // The forward loads a row's vectors straight into registers: a thread has nothing else to keep, so four CTAs of a 4096-element
 // row share an SM and their loads lie under one another.  (The backward's ring took 101 us here instead of 89, 16384 x 4096.)
@@ -344,7 +379,7 @@ __global__ void __launch_bounds__(fwd_threads(V, ITEMS, S), fwd_ctas(V, ITEMS, S
 template <class T, class W, int V, int ITEMS, Span S, bool SHIFT>
 __global__ void __launch_bounds__(BWD_THREADS) norm_bwd_kernel(const NormArgs a) {
   constexpr int RING = ring_of(V);
-  __shared__ float red[RED_FLOATS];
+  __shared__ __align__(8) float red[S == TEAM ? 2 * RED_FLOATS : RED_FLOATS];
   extern __shared__ uint4 ring_mem[];
   const Place<V, ITEMS, S, SHIFT> at(a);
   const Ring<T, 3, V, ITEMS, S, SHIFT> ring{ring_mem, at, (int64_t)a.T * a.D, ring_mem + RING * 3 * ITEMS * blockDim.x};
@@ -375,16 +410,10 @@ __global__ void __launch_bounds__(BWD_THREADS) norm_bwd_kernel(const NormArgs a)
 #pragma unroll
     for (int e = 0; e < H; ++e) dw[i][e] = db[i][e] = 0ull;
   }
-  int turn = 0, k = 0;
-  int64_t row = at.row;
-  for (int64_t done = 0; done < a.T; done += at.step, row += at.step, k = k + 1 == RING ? 0 : k + 1) {
-    const bool ok = row < a.T;
-    const float rs = next_rstd, minus = -next_mean * next_rstd;
+  // the products that a row's two sums are made of, and the columns' sums; `y` and `h` of the row stay in ry, rh
+  auto products = [&](int k, bool ok, float rs, float minus, Raw<T, V> (&ry)[ITEMS], Raw<T, V> (&rh)[ITEMS], float (&s)[2]) {
     const uint64_t rs2 = pack_f32x2(rs, rs), minus2 = pack_f32x2(minus, minus);
-    request_stats(row + at.step);
-    Raw<T, V> ry[ITEMS], rh[ITEMS];   // (as vectors of the element type they take half the registers across the joining of the sums)
     uint64_t s0 = 0ull, s1 = 0ull;
-    copies_wait_first<RING>();
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
       float y[V], u[V], w[V];
@@ -403,12 +432,14 @@ __global__ void __launch_bounds__(BWD_THREADS) norm_bwd_kernel(const NormArgs a)
         db[i][e] = add_f32x2(y2, db[i][e]);
       }
     }
-    float s[2], p, q;
+    float p, q;
     unpack_f32x2(s0, p, q);
     s[0] = p + q;
     unpack_f32x2(s1, p, q);
     s[1] = p + q;
-    row_sum<S>(s, at.tpr, at.sub, a.team, red, turn);
+  };
+  auto finish = [&](int k, int64_t row, bool ok, float rs, float minus, const Raw<T, V> (&ry)[ITEMS], const Raw<T, V> (&rh)[ITEMS], const float (&s)[2]) {
+    const uint64_t rs2 = pack_f32x2(rs, rs), minus2 = pack_f32x2(minus, minus);
     const float c2 = -s[0] * a.inv_d * rs, c1 = a.rms ? 0.f : -s[1] * a.inv_d * rs;
     const uint64_t c22 = pack_f32x2(c2, c2), c12 = pack_f32x2(c1, c1);
 #pragma unroll
@@ -433,6 +464,51 @@ __global__ void __launch_bounds__(BWD_THREADS) norm_bwd_kernel(const NormArgs a)
       if (ok) at.store(i, dx + row * a.D, o);
     }
     copy_row(k, row + RING * at.step);   // (after this thread's reads of the slot)
+  };
+  Raw<T, V> ry[ITEMS], rh[ITEMS];   // (as vectors of the element type they take half the registers across the joining of the sums)
+  int64_t row = at.row;
+  if constexpr (S == TEAM && RING == 4) {
+    // The cluster's exchange of one row lies under the products of the next: arrive(r), then row r - 1 is finished, then the products of
+    // row r + 1, and only then wait(r).  Four buffers of sums: one is written again when every CTA has arrived once more after its last
+    // reads of it.
+    float was_rs = 0.f, was_minus = 0.f;
+    int n = 0;
+    for (int64_t done = 0;; done += at.step, row += at.step, ++n) {
+      const bool more = done < a.T;   // (the same in all CTAs of a cluster)
+      const float rs = next_rstd, minus = -next_mean * next_rstd;
+      float s[2];
+      if (more) {
+        request_stats(row + at.step);
+        copies_wait_first<RING - 1>();   // row n's: RING + n - 1 have been asked for, RING at first
+        products(n % RING, row < a.T, rs, minus, ry, rh, s);
+        team_put(s, red + n % 4 * 64);
+      }
+      if (n > 0) cluster_wait();
+      if (more) cluster_arrive();
+      if (n > 0) {
+        const int k = (n - 1) % RING;
+        const int64_t was = row - at.step;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) { ring.read(k, 0, i, was < a.T, ry[i]); ring.read(k, 1, i, was < a.T, rh[i]); }
+        team_get(s, red + (n - 1) % 4 * 64, at.tpr >> 5, a.team);
+        finish(k, was, was < a.T, was_rs, was_minus, ry, rh, s);
+      }
+      if (!more) break;
+      was_rs = rs;
+      was_minus = minus;
+    }
+  } else {
+    int turn = 0, k = 0;
+    for (int64_t done = 0; done < a.T; done += at.step, row += at.step, k = k + 1 == RING ? 0 : k + 1) {
+      const bool ok = row < a.T;
+      const float rs = next_rstd, minus = -next_mean * next_rstd;
+      float s[2];
+      request_stats(row + at.step);
+      copies_wait_first<RING>();
+      products(k, ok, rs, minus, ry, rh, s);
+      row_sum<S>(s, at.tpr, at.sub, a.team, red, turn);
+      finish(k, row, ok, rs, minus, ry, rh, s);
+    }
   }
   copies_wait_all();
   if (S == TEAM) tc::cluster_sync();   // no CTA leaves while the other one may still read its sums

@@ -322,3 +322,16 @@ def test_supplied_outputs_without_a_residual_return_x_as_h(rms):
     assert got[1] is i["x"] and (buffer == 7.0).all()
     for a, b in zip(got, want):
         assert (a is None and b is None) or torch.equal(a, b)
+
+
+@pytest.mark.parametrize("T, D, dt", [(1531, 16384, BF16), (700, 9000, FP16), (333, 32768, BF16), (300, 16383, BF16), (400, 16384, FP32)])
+def test_clusters_give_the_same_bits_every_time(T, D, dt):
+    """Rows that a cluster shares: the sums that its CTAs read from one another are complete and of the right row."""
+    i = _inputs(T, D, dt, dt)
+    first = None
+    for _ in range(25):
+        y, h, mean, rstd = binding.bdlm_norm_fwd(i["x"], i["w"], i["b"], i["res"])
+        got = (y, h, mean, rstd) + binding.bdlm_norm_bwd(i["dy"], h, i["w"], mean, rstd, dh=i["dh"], bias=True)
+        first = got if first is None else first
+        assert all(torch.equal(a, b) for a, b in zip(got, first))
+    _check_backward(first[4:], i, first[1], first[2], first[3], i["w"], i["dh"], True, False, dt, dt)
