@@ -36,13 +36,13 @@ __device__ __forceinline__ int ld_cluster_int(const int* own, int rank) {
 __device__ __forceinline__ void wait_for_sort() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
-// What a thread of a group of `tpr` has of a row's slab: a vector, or, where rows are no whole number of those, eight single elements
+// What a thread of a group of `tpr` has of a row's slab: a vector, or, where rows are no whole number of those, S single elements
 // tpr apart.
-template <class T, int V>
+template <class T, int V, int S>
 struct Slice {
-  static constexpr int C = V > 1 ? V : 8;
-  Raw<T, V> q[V > 1 ? 1 : 8];
-  __device__ __forceinline__ static int first(int slab, int tpr, int lane) { return V > 1 ? (slab * tpr + lane) * V : slab * 8 * tpr + lane; }   // its first column
+  static constexpr int C = V > 1 ? V : S;
+  Raw<T, V> q[V > 1 ? 1 : S];
+  __device__ __forceinline__ static int first(int slab, int tpr, int lane) { return V > 1 ? (slab * tpr + lane) * V : slab * S * tpr + lane; }   // its first column
   __device__ __forceinline__ void load(const T* row, int at, int tpr, int D) {
     if (V > 1) { q[0].load(row + at); return; }
 #pragma unroll
@@ -274,6 +274,7 @@ struct SumArgs {
   int T, D, V, piece, pieces, slabs, tpr;
   float scale;
   int accumulate;
+  int spread;      // neighbouring pieces in different CTAs
 };
 
 constexpr int SUM_THREADS = 512, GROUP_THREADS = 128;   // threads of a CTA; of a piece's slab, at most
@@ -291,9 +292,33 @@ __device__ __forceinline__ void zero_row(E* row, int D) {
   if (tail + lane < D) row[tail + lane] = E(0.f);
 }
 
+// The same for n short rows that lie one after the other, of which absent(r) says whether row r is to be zeroed: by the vectors that
+// cover them, a thread each, where a warp to a row would leave most of its lanes idle.  (91650 rows of 154 bytes: the call 17 us instead
+// of 27, in part by more tokens in flight; 128256 rows of 384 bytes 32 instead of 29.)
+constexpr int SHORT_ROW = 256;   // bytes
+template <class E, class F>
+__device__ __forceinline__ void zero_short_rows(E* rows, int n, int D, F absent) {
+  constexpr int PER = 16 / (int)sizeof(E);
+  const int shift = (int)((uintptr_t)rows & 15u) / (int)sizeof(E), total = n * D;
+  for (int v = threadIdx.x; v * PER < total + shift; v += blockDim.x) {
+    const int first = v * PER - shift, lo = max(first, 0), hi = min(first + PER, total);
+    int r = lo / D;
+    const int last = (hi - 1) / D;
+    bool all = hi - lo == PER;
+    for (int q = r; q <= last; ++q) all = all && absent(q);
+    if (all) { *reinterpret_cast<uint4*>(rows + first) = make_uint4(0u, 0u, 0u, 0u); continue; }
+    int end = (r + 1) * D;   // of the element's row
+    for (int e = lo; e < hi; ++e) {
+      if (e == end) { ++r; end += D; }
+      if (absent(r)) rows[e] = E(0.f);
+    }
+  }
+}
+
 // E: table, O: tokens' rows.  A group of `tpr` threads takes a piece and a slab of columns, a Slice of it each.
 // FEW: no more than FEW_TOKENS of them, one piece: each CTA sorts them itself, and this is the only launch.
 constexpr int FEW_TOKENS = 32;
+__host__ __device__ constexpr int singles(bool few) { return few ? 2 : 8; }   // of a Slice: few tokens are a chain of loads, and threads there are enough
 template <class E, class O, int V, bool ADD, bool FEW>
 __global__ void __launch_bounds__(SUM_THREADS, 2) embed_sum_kernel(const SumArgs a) {
   __shared__ uint32_t present[FILL_WORDS];
@@ -311,8 +336,11 @@ __global__ void __launch_bounds__(SUM_THREADS, 2) embed_sum_kernel(const SumArgs
         if (at >= 0 && at < n) atomicOr(&present[at >> 5], 1u << (at & 31));
       }
       __syncthreads();
-      for (int r = threadIdx.x >> 5; r < n; r += SUM_THREADS / 32)
-        if (!((present[r >> 5] >> (r & 31)) & 1u)) zero_row(dtable + (v0 + r) * a.D, a.D);
+      auto absent = [&](int r) { return !((present[r >> 5] >> (r & 31)) & 1u); };
+      if (a.D * (int)sizeof(E) <= SHORT_ROW) zero_short_rows(dtable + v0 * a.D, n, a.D, absent);
+      else
+        for (int r = threadIdx.x >> 5; r < n; r += SUM_THREADS / 32)
+          if (absent(r)) zero_row(dtable + (v0 + r) * a.D, a.D);
       __syncthreads();
     }
   }
@@ -337,9 +365,11 @@ __global__ void __launch_bounds__(SUM_THREADS, 2) embed_sum_kernel(const SumArgs
   const O* dout = static_cast<const O*>(a.dout);
   const int groups = SUM_THREADS / a.tpr, lane = threadIdx.x % a.tpr;
   const int64_t items = (int64_t)a.pieces * a.slabs;
-  for (int64_t item = (int64_t)blockIdx.x * groups + threadIdx.x / a.tpr; item < items; item += (int64_t)gridDim.x * groups) {
-    using Row = Slice<O, V>;
-    using Out = Slice<E, V>;
+  const int group = threadIdx.x / a.tpr;
+  const int64_t begin_item = a.spread ? (int64_t)group * gridDim.x + blockIdx.x : (int64_t)blockIdx.x * groups + group;
+  for (int64_t item = begin_item; item < items; item += (int64_t)gridDim.x * groups) {
+    using Row = Slice<O, V, singles(FEW)>;
+    using Out = Slice<E, V, singles(FEW)>;
     constexpr int N = Row::C;
     const int p = (int)(item / a.slabs), col = Row::first((int)(item % a.slabs), a.tpr, lane);
     const int64_t first = (int64_t)p * a.piece, last = min((int64_t)a.T, first + a.piece);
@@ -352,7 +382,9 @@ __global__ void __launch_bounds__(SUM_THREADS, 2) embed_sum_kernel(const SumArgs
     const bool follow = end == after && end != before && far_after != end;
     float acc[N];
     int run = -1;
-    constexpr int U = V == 1 || ADD ? 2 : 4;   // tokens in flight: what 64 registers hold
+    // tokens in flight: what 64 registers hold.  (32 tokens of 1001 elements, added: 43 us, with more of them 16; vectors, which would
+    // have to spill for it, lose: 14 tokens of 6864 11 us, 16.)
+    constexpr int U = FEW && V == 1 ? (ADD ? 4 : 8) : V == 1 || ADD ? 2 : 4;
     const int64_t most = follow ? min((int64_t)a.T, last + a.piece) : last;
     for (int64_t i = first; i < most; i += U) {
       int2 pr[U + 1];
@@ -406,7 +438,7 @@ __global__ void __launch_bounds__(SUM_THREADS, 2) embed_sum_kernel(const SumArgs
 // ------------------------------------------------------------------------------------------------ join
 // Long runs.  The piece in which such a run begins has it in its second part, the ones after it in their first.
 // A CTA takes 32 C columns of the runs that begin in every gridDim.y-th piece; its warps add the parts in turn.
-constexpr int JOIN_WARPS = 16, JOIN_Y = 16;
+constexpr int JOIN_WARPS = 16, JOIN_Y = 16, JOIN_CTAS = 256;   // JOIN_Y or more CTAs share the pieces, JOIN_CTAS in all where columns are few
 template <class E, int C>
 __global__ void __launch_bounds__(JOIN_WARPS * 32) embed_join_kernel(const SumArgs a) {
   __shared__ float sums[JOIN_WARPS][32 * C + 1];
@@ -576,15 +608,19 @@ int bdlm_embed_bwd(const bdlm_embed_params* p, const void* dout, const int32_t* 
     }
     if (e != cudaSuccess) return BDLM_ERR_CUDA;
   }
-  const int V = vector_of(p), slices = V > 1 ? p->D / V : (p->D + 7) / 8;
+  const int V = vector_of(p), slices = V > 1 ? p->D / V : (p->D + singles(few) - 1) / singles(few);
   SumArgs a = {};
   a.dout = dout; a.ids = ids; a.sorted = sorted; a.dtable = dtable;
   a.parts = reinterpret_cast<float*>(ws + 2 * pairs_bytes(p->T));
   a.T = p->T; a.D = p->D; a.V = p->V; a.piece = piece_of(p->T); a.pieces = pieces_of(p->T);
-  a.tpr = pow2_at_least(slices, GROUP_THREADS); a.slabs = (slices + a.tpr - 1) / a.tpr;
+  // Where a warp would hold many pieces, which diverge, and few CTAs all of them: a warp to a piece, and pieces spread over the CTAs.
+  // (8000 tokens of 7 elements 63 us, so 32; 4000 of 320, no longer so, 30, so 33.)
+  a.spread = slices < 8;
+  a.tpr = a.spread ? 32 : pow2_at_least(slices, GROUP_THREADS);
+  a.slabs = (slices + a.tpr - 1) / a.tpr;
   a.scale = p->scale; a.accumulate = p->accumulate;
   const int64_t items = (int64_t)a.pieces * a.slabs, groups = SUM_THREADS / a.tpr;
-  int64_t want = (items + groups - 1) / groups;
+  int64_t want = a.spread ? items : (items + groups - 1) / groups;
   if (!a.accumulate && want < ((int64_t)p->V + 15) / 16) want = ((int64_t)p->V + 15) / 16;
   const int64_t cap = (int64_t)device_sm_count() * 2;
   const unsigned blocks = (unsigned)(want < cap ? want : cap);
@@ -602,7 +638,8 @@ int bdlm_embed_bwd(const bdlm_embed_params* p, const void* dout, const int32_t* 
     if (e != cudaSuccess || a.pieces < 2) return;
     const int cols = p->D % 4 == 0 ? 128 : 32;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((p->D + cols - 1) / cols), (unsigned)(a.pieces - 1 < JOIN_Y ? a.pieces - 1 : JOIN_Y));
+    const int gx = (p->D + cols - 1) / cols, gy = JOIN_CTAS / gx > JOIN_Y ? JOIN_CTAS / gx : JOIN_Y;
+    cfg.gridDim = dim3((unsigned)gx, (unsigned)(a.pieces - 1 < gy ? a.pieces - 1 : gy));
     cfg.blockDim = dim3(JOIN_WARPS * 32);
     cfg.stream = st;
     cudaLaunchAttribute attr = {};

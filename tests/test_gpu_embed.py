@@ -301,3 +301,20 @@ def test_refusals():
     assert e.value.status == -3
     with pytest.raises(AssertionError):
         binding.bdlm_embed_fwd(table[:, ::2], ids)
+
+
+@pytest.mark.parametrize("e", [BF16, FP32])
+@pytest.mark.parametrize("D", [1, 2, 5, 7, 31, 55, 56, 63, 64, 65, 120, 127, 128, 129])
+def test_short_rows_and_what_lies_behind_the_table(D, e):
+    """Rows that are zeroed by the vectors that cover them and the longer ones beside them, shares of CTAs that begin and end anywhere in
+    a vector, one launch and three; memory behind the table stays as it was."""
+    for T, V in ((3, 1), (32, 297), (33, 593), (300, 10007), (1000, 128256)):
+        _check_bwd(T, D, V, e, e, masked=0.2)
+        _check_bwd(T, D, V, e, e, masked=0.2, start=True)
+        buffer = torch.full((V * D + 64,), 7.0, dtype=e, device="cuda")
+        ids = _ids(T, V, D)
+        dout = torch.randn(T, D, generator=torch.Generator().manual_seed(D)).to(e).cuda()
+        binding.bdlm_embed_bwd(dout, torch.from_numpy(ids).int().cuda(), V, out=buffer[:V * D].view(V, D))
+        assert (buffer[V * D:] == 7.0).all()
+        absent = np.setdiff1d(np.arange(V), ids)
+        assert (buffer[:V * D].view(V, D)[torch.from_numpy(absent).cuda()] == 0).all()
