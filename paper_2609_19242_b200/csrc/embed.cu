@@ -12,8 +12,8 @@
 //           piece leaves an fp32 part.  (With parts of every run that crosses a border, a third of the borders of 16384 tokens
 //           over 32008 ids had some, and joining them took 25 us of 85.)
 //   join    adds the parts of such long runs (the mask token's covers hundreds of pieces)
-// Every sum runs in the tokens' order inside a piece, and a long run's over its pieces in sixteen interleaved shares that are added in
-// order: the ids alone fix the order, and no atomics meet in a sum.
+// Every sum runs in the tokens' order inside a piece, and a long run's over its pieces in order, or in
+// sixteen interleaved shares that are added in order: the ids alone fix the order, and no atomics meet in a sum.
 #include <math.h>
 
 #include "../../include/bdlm_embed.h"
@@ -437,12 +437,15 @@ __global__ void __launch_bounds__(SUM_THREADS, 2) embed_sum_kernel(const SumArgs
 
 // ------------------------------------------------------------------------------------------------ join
 // Long runs.  The piece in which such a run begins has it in its second part, the ones after it in their first.
-// A CTA takes 32 C columns of the runs that begin in every gridDim.y-th piece; its warps add the parts in turn.
-constexpr int JOIN_WARPS = 16, JOIN_Y = 16, JOIN_CTAS = 256;   // JOIN_Y or more CTAs share the pieces, JOIN_CTAS in all where columns are few
+// A CTA takes 32 C columns of the runs that begin in every gridDim.y-th piece.  Words of a text occur so unevenly that a batch has dozens of
+// them, most of a few pieces: each of those is one warp's, so that they are added beside one another.  A longer one's parts are added
+// by all warps in turn.  (8192 x 4096, the ids' logarithms even: the call 101 us with all warps for every run, 89 so.)
+constexpr int JOIN_WARPS = 16, JOIN_Y = 16, JOIN_CTAS = 256, WARP_PARTS = 10;   // JOIN_Y or more CTAs share the pieces, JOIN_CTAS in all where columns are few
 template <class E, int C>
 __global__ void __launch_bounds__(JOIN_WARPS * 32) embed_join_kernel(const SumArgs a) {
   __shared__ float sums[JOIN_WARPS][32 * C + 1];
   __shared__ int2 runs[JOIN_WARPS * 32];   // id, first piece
+  __shared__ int ends[JOIN_WARPS * 32];    // and its last
   __shared__ int count;
   if (threadIdx.x == 0) count = 0;
   wait_for_predecessor();
@@ -461,27 +464,49 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) embed_join_kernel(const SumAr
     }
   }
   __syncthreads();
-  for (int i = 0; i < count; ++i) {
+  auto add = [&](float (&s)[C], int64_t part) {
+    Raw<float, C> r;
+    float f[C];
+    r.load(a.parts + part * a.D + c);
+    r.get(f);
+#pragma unroll
+    for (int e = 0; e < C; ++e) s[e] += f[e];
+  };
+  // A warp to a run: the last piece that begins with it, in two looks (every 32nd piece, then 32 pieces), and the sum of one of few parts.
+  for (int i = warp; i < count; i += JOIN_WARPS) {
     const int2 run = runs[i];
-    // the last piece that begins with it, in two looks of a warp: every 32nd piece, then 32 pieces
     auto begins = [&](int q) { return q < a.pieces && key((int64_t)q * a.piece) == run.x; };
     int last = run.y + 32 * __popc(__ballot_sync(0xffffffffu, begins(run.y + 32 * (lane + 1))));
     last += __popc(__ballot_sync(0xffffffffu, begins(last + 1 + lane)));
+    if (lane == 0) ends[i] = last;
+    if (last - run.y > WARP_PARTS || c >= a.D) continue;
+    float s[C], g[C];
+#pragma unroll
+    for (int e = 0; e < C; ++e) s[e] = 0.f;
+    E* at = dtable + (int64_t)run.x * a.D + c;
+    Raw<E, C> old, o;
+    if (a.accumulate) old.load(at);
+    add(s, (int64_t)run.y * 2 + 1);
+#pragma unroll 8
+    for (int q = run.y + 1; q <= last; ++q) add(s, (int64_t)q * 2);
+    if (a.accumulate) old.get(g);
+#pragma unroll
+    for (int e = 0; e < C; ++e) s[e] = a.accumulate ? fmaf(s[e], a.scale, g[e]) : s[e] * a.scale;
+    o.put(s);
+    o.store(at);
+  }
+  __syncthreads();
+  for (int i = 0; i < count; ++i) {   // the longer ones, by all warps
+    const int2 run = runs[i];
+    const int last = ends[i];
+    if (last - run.y <= WARP_PARTS) continue;
     float s[C];
 #pragma unroll
     for (int e = 0; e < C; ++e) s[e] = 0.f;
     if (c < a.D) {
-      auto add = [&](int64_t part) {
-        Raw<float, C> r;
-        float f[C];
-        r.load(a.parts + part * a.D + c);
-        r.get(f);
-#pragma unroll
-        for (int e = 0; e < C; ++e) s[e] += f[e];
-      };
-      if (warp == 0) add((int64_t)run.y * 2 + 1);
+      if (warp == 0) add(s, (int64_t)run.y * 2 + 1);
 #pragma unroll 8
-      for (int q = run.y + 1 + warp; q <= last; q += JOIN_WARPS) add((int64_t)q * 2);
+      for (int q = run.y + 1 + warp; q <= last; q += JOIN_WARPS) add(s, (int64_t)q * 2);
     }
 #pragma unroll
     for (int e = 0; e < C; ++e) sums[warp][lane * C + e] = s[e];

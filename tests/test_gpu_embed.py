@@ -1,8 +1,8 @@
 """The token embedding against its fp64 oracle, through the binding.
 
 Tolerances.  The lookup is one fp32 product rounded once: (eps/2 + 2^-24) of the value.  A gradient row of n tokens is summed in
-fp32: at most 2 `piece` additions one after the other (piece: 8, or T / 1024), or `piece` of them and then the pieces' parts
-in sixteen shares, so for the sizes here it is off by at most (piece + T / (8 piece) + 16) x 2^-24 of the sum of the terms'
+fp32: at most 2 `piece` additions one after the other (piece: 8, or T / 1024), or `piece` of them and then the parts of up to 11
+pieces in order, or of more in sixteen shares, so for the sizes here it is off by at most (piece + T / (8 piece) + 16) x 2^-24 of the sum of the terms'
 magnitudes (2 piece is less for T up to 147000), and rounded once."""
 import numpy as np
 import pytest
@@ -318,3 +318,16 @@ def test_short_rows_and_what_lies_behind_the_table(D, e):
         assert (buffer[V * D:] == 7.0).all()
         absent = np.setdiff1d(np.arange(V), ids)
         assert (buffer[:V * D].view(V, D)[torch.from_numpy(absent).cuda()] == 0).all()
+
+
+@pytest.mark.parametrize("D", [33, 40, 264])
+@pytest.mark.parametrize("start", [None, True])
+def test_runs_of_every_number_of_pieces(D, start):
+    """Runs of 2 to 30 pieces of eight tokens, which begin and end anywhere in a piece: a warp adds the parts of the shorter ones, a
+    whole CTA those of the longer ones."""
+    rng = np.random.default_rng(D)
+    lengths = rng.permutation(np.concatenate([np.arange(1, 250, 7), np.arange(8, 100, 8), [1] * 40]))
+    ids = rng.permutation(np.repeat(np.arange(len(lengths)) * 3, lengths))
+    assert len(ids) < 8192
+    _check_bwd(len(ids), D, 3 * len(lengths), FP32, FP32, ids=ids, start=start)
+    _check_bwd(len(ids), D, 3 * len(lengths), BF16, BF16, ids=ids, scale=0.25, start=start)
