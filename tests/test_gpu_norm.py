@@ -335,3 +335,46 @@ def test_clusters_give_the_same_bits_every_time(T, D, dt):
         first = got if first is None else first
         assert all(torch.equal(a, b) for a, b in zip(got, first))
     _check_backward(first[4:], i, first[1], first[2], first[3], i["w"], i["dh"], True, False, dt, dt)
+
+
+FAR = [(1, 100, FP32), (300, 100, FP32), (300, 333, FP32), (1, 4096, FP32), (300, 1544, FP32), (300, 4096, FP32), (300, 4095, FP32),
+       (300, 16384, FP32), (300, 16383, FP32), (300, 100, BF16), (300, 4096, BF16), (300, 4095, FP16), (300, 12000, BF16), (300, 16383, FP16)]
+
+
+def _far(T, D, dt):
+    """Rows whose mean is a thousand times their deviation (16-bit rows, which hold no more: a hundred times)."""
+    g = torch.Generator().manual_seed(T + D)
+    x = (torch.randn(T, D, generator=g) + (1000.0 if dt == FP32 else 100.0)).to(dt).cuda()
+    w = (1 + 0.2 * torch.randn(D, generator=g)).cuda()
+    _, _, mean, rstd = binding.bdlm_norm_fwd(x, w)
+    n = (_f64(x) - _f64(mean)[:, None]) * _f64(rstd)[:, None]
+    return x, w, mean, rstd, n, g
+
+
+@pytest.mark.parametrize("T, D, dt", FAR)
+def test_normalised_values_of_the_backward_far_from_a_zero_mean(T, D, dt):
+    """n = (h - mean) rstd is formed as it stands: a subtraction and a product, each off by half a step (2^-24 of the value), however
+    far the mean lies from zero.  With a gradient of ones in one row alone dweight is that row's n: all else that is added to it is zero."""
+    x, w, mean, rstd, n, _ = _far(T, D, dt)
+    for row in sorted({0, T // 2, T - 1}):
+        dy = torch.zeros_like(x)
+        dy[row] = 1.0
+        _, dw, db = binding.bdlm_norm_bwd(dy, x, w, mean, rstd, bias=True)
+        assert (db == 1.0).all()
+        assert (np.abs(_f64(dw) - n[row]) <= 2.0 ** -23 * np.abs(n[row]) + 1e-30).all()
+
+
+@pytest.mark.parametrize("T, D, dt", FAR)
+def test_gradient_of_rows_far_from_a_zero_mean(T, D, dt):
+    """The sums' errors are those of the head of this file, n's those of the test above."""
+    x, w, mean, rstd, n, gen = _far(T, D, dt)
+    dy = (0.5 + torch.rand(T, D, generator=gen)).to(dt).cuda()
+    dx, dw, _ = binding.bdlm_norm_bwd(dy, x, w, mean, rstd)
+    rx, rw, _ = orc.norm_backward(_f64(dy), _f64(x), _f64(w), _f64(mean), _f64(rstd), None, False)
+    r, g, dn = _f64(rstd)[:, None], _f64(dy) * _f64(w), 2.0 ** -23 * np.abs(n)
+    mean_of = lambda t: t.mean(axis=1, keepdims=True)
+    off = r * (SLACK * (np.abs(g) + mean_of(np.abs(g)) + np.abs(n) * mean_of(np.abs(g * n))) + dn * mean_of(np.abs(g * n)) +
+               np.abs(n) * mean_of(np.abs(g) * dn))
+    assert (np.abs(_f64(dx) - rx) <= _half_ulp(dt) * (np.abs(rx) + off) + off).all()
+    ow = (T / 148 + 150) * 2.0 ** -24 * np.abs(_f64(dy) * n).sum(axis=0) + (np.abs(_f64(dy)) * dn).sum(axis=0)
+    assert (np.abs(_f64(dw) - rw) <= ow).all()
