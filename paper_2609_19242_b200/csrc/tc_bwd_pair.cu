@@ -295,6 +295,10 @@ tc_bwd_pair_kernel(const __grid_constant__ PairMaps maps, const KArgs a, const T
           b0 = b1; b1 = b2; b2 = t;
         }
         if (DQ && ok) {
+          // dQ^T of the last step waits for no dP^T.  This warp, which has waited for all phases before it, arrives in the compute
+          // warps' place: those of one CTA, a step's end ahead of the other one's, would have completed the phase before this one,
+          // and dQ^T of the last step but one went over dP^T that the other CTA was still reading.
+          if (lane == 0) mbar_arrive_n(bar_go_dq, 16);
           ok = go(bar_go_dq, nsteps - 1, w_dq);
           if (ok) issue_dqt();
         }
@@ -558,7 +562,6 @@ tc_bwd_pair_kernel(const __grid_constant__ PairMaps maps, const KArgs a, const T
       if (lane == 0) { mbar_arrive_peer(r_go_dk); if (DQ) mbar_arrive(bar_dsl); mbar_arrive(bar_rows_empty + 8 * sr); }   // this warp is done with the stage's LSE / D rows
       c_ds += tick<TR>() - t2;
     }
-    if (DQ && ok && lane == 0 && nsteps > 0) mbar_arrive_peer(r_go_dq);   // dQ^T of the last step waits for no dP^T
     if (warp == 0 && lane == 0 && rank == 0) {
       trace_add(a.trace, 16 + 0, nsteps); trace_add(a.trace, 16 + 1, w_st); trace_add(a.trace, 16 + 2, w_dpt);
       trace_add(a.trace, 16 + 3, w_dsf); trace_add(a.trace, 16 + 4, c_exp); trace_add(a.trace, 16 + 5, c_ds);
