@@ -117,8 +117,9 @@ int bdlm_attn_fwd(const bdlm_params* p,
  * is fixed, so they are bitwise reproducible; dQ is too on the two-pass path, and reproducible up to
  * fp32 summation order when the fused kernel runs (see bdlm_params.bwd_single_pass for which one
  * does).  Requires the full clean key range.
- * NaN and infinities among the inputs: hidden elements with finite values have no effect, but the products run over
- * whole tiles, and there a hidden zero times a NaN is NaN.  A NaN in a query's row (q, do, o, lse) can reach dK / dV of
+ * NaN and infinities among the inputs (o and lse are inputs too): hidden elements with finite values have no effect, as long as the
+ * products with them are finite: dO . V of a hidden pair, and its difference from D, must not overflow fp32 (rows of 128
+ * elements below 1e18 cannot).  The forward has no such bound.  The products run over whole tiles, and there a hidden zero times a NaN is NaN.  A NaN in a query's row (q, do, o, lse) can reach dK / dV of
  * keys that the row does not see, and one in a key's row dQ of queries that do not see it, up to 256 positions away
  * (128 where one CTA takes each key tile: short calls, head dimension 64).  With gathered K/V (kv_chunk_len, an odd
  * number of 128-row tiles) a pair of CTAs may join the end of one chunk and the beginning of the next in memory; for
@@ -231,7 +232,8 @@ int bdlm_attn_bwd_packed(const bdlm_params* p, const bdlm_packed_geometry* g,
  *     non-decreasing int32 in [0, L] (empty documents are allowed); its values are not validated, wrong ones give wrong
  *     masks but no access outside the tensors.  Positions before the first and from the last entry on belong to no document:
  *     clean rows there see nothing (O = 0, LSE = -inf, zero gradients).
- *   - Finite values of one document have no effect on another, but the products run over whole tiles, and there a hidden zero
+ *   - Finite values of one document have no effect on another, in the backward as long as its o and lse and the products with them are
+ *     finite too (see bdlm_attn_bwd), but the products run over whole tiles, and there a hidden zero
  *     times a NaN or an infinity is NaN: from one document, or from positions of none, it can reach rows of its neighbours up to 256
  *     positions away.  All rows have to hold finite values.
  *   - With q_noisy NULL this is causal attention over prompts of different lengths (block_size is then unused: pass 1).
