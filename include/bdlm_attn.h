@@ -226,7 +226,10 @@ int bdlm_attn_bwd_packed(const bdlm_params* p, const bdlm_packed_geometry* g,
  *     cu_seqlens[i] .. cu_seqlens[i + 1] - 1.  Every rule above applies inside a document: a clean query sees the clean
  *     keys of its own document only (of any length, one token included), and a corrupted block belongs to the document
  *     of the position it starts at, block_prefix[b], and sees that document's clean keys before it (none, where
- *     block_prefix[b] is the document's first position).  Position L belongs to no document.
+ *     block_prefix[b] is the document's first position).  Position L belongs to no document.  A block's own rows see one another
+ *     whatever lies between them, so with block_prefix NULL (blocks one after the other over the positions) the documents have to be
+ *     whole numbers of blocks: one that a border cuts would mix two documents, or a document and positions of none.  The
+ *     library does not see the lengths and does not check this.
  *   - bdlm_doc_table writes the table that the kernels read, once for a packed batch; the layers' calls, forward and
  *     backward, share it.  It is the same for all batch elements.  cu_seqlens is a DEVICE array of n_docs + 1
  *     non-decreasing int32 in [0, L] (empty documents are allowed); its values are not validated, wrong ones give wrong

@@ -373,12 +373,24 @@ def _packed_setup(q_clean, k_clean, q_noisy, block_size, block_prefix, clean_q_p
 
 class DocTable:
     """The table of a packed batch's documents (bdlm_doc_table): `table` int32 [L + 1, 2] on the device (each position's
-    document), `struct` what the library is handed.  One table serves every layer's forward and backward of the batch."""
+    document), `struct` what the library is handed, `borders` where documents begin and end (host int64, None: not known).  One
+    table serves every layer's forward and backward of the batch."""
 
-    def __init__(self, buffer, L, max_len, pairs):
-        self.buffer, self.L, self.max_len, self.pairs = buffer, L, max_len, pairs
+    def __init__(self, buffer, L, max_len, pairs, borders=None):
+        self.buffer, self.L, self.max_len, self.pairs, self.borders = buffer, L, max_len, pairs, borders
         self.table = buffer[:2 * (L + 1)].view(L + 1, 2)
         self.struct = BdlmDocs(buffer.data_ptr(), max_len, 0, pairs)
+        self._cut = {}
+
+    def first_cut(self, block_size, rows):
+        """The first document border inside one of the blocks that lie one after the other over the first `rows` positions, or None."""
+        if self.borders is None:
+            return None
+        key = (block_size, rows)
+        if key not in self._cut:
+            inside = self.borders[(self.borders % block_size != 0) & (self.borders < rows)]
+            self._cut[key] = int(inside.min()) if inside.numel() else None
+        return self._cut[key]
 
 
 def bdlm_doc_table(cu_seqlens, L=None, device=None) -> DocTable:
@@ -403,10 +415,11 @@ def bdlm_doc_table(cu_seqlens, L=None, device=None) -> DocTable:
         rc = lib().bdlm_doc_table(_ptr(dev), dev.numel() - 1, L, _ptr(buffer), _stream())
     if rc != 0:
         raise BdlmError(rc, "bdlm_doc_table")
-    return DocTable(buffer, L, int(lens.max()), int((lens * (lens + 1) // 2).sum()))
+    some = lens > 0
+    return DocTable(buffer, L, int(lens.max()), int((lens * (lens + 1) // 2).sum()), torch.cat([host[:-1][some], host[1:][some]]))
 
 
-def _check_docs(docs, k_clean, kv_chunks):
+def _check_docs(docs, k_clean, kv_chunks, q_noisy, block_size, block_prefix):
     index = _current(k_clean)
     if docs.L != k_clean.shape[1]:
         raise ValueError("the table of documents is for another number of clean positions")
@@ -414,6 +427,11 @@ def _check_docs(docs, k_clean, kv_chunks):
         raise ValueError("the table of documents is on another device")
     if kv_chunks is not None:
         raise ValueError("documents and gathered clean K/V (kv_chunks) cannot be combined")
+    if q_noisy is not None and block_prefix is None:
+        cut = docs.first_cut(block_size, q_noisy.shape[1])
+        if cut is not None:   # the rows of a block see one another, so those of two documents would
+            raise ValueError(f"a document begins or ends at position {cut}, inside a block of {block_size}: without block_prefix documents "
+                             "must be whole numbers of blocks")
 
 
 def bdlm_attn_fwd_packed(q_clean, k_clean, v_clean, q_noisy, k_noisy, v_noisy, block_size, *,
@@ -426,7 +444,7 @@ def bdlm_attn_fwd_packed(q_clean, k_clean, v_clean, q_noisy, k_noisy, v_noisy, b
     with q_noisy None and block_size 1 that is causal attention over prompts of different lengths.
     Returns (o_clean, lse_clean, o_noisy, lse_noisy)."""
     if docs is not None:
-        _check_docs(docs, k_clean, kv_chunks)
+        _check_docs(docs, k_clean, kv_chunks, q_noisy, block_size, block_prefix)
     p, g = _packed_setup(q_clean, k_clean, q_noisy, block_size, block_prefix, clean_q_pos0, window, kv_chunks,
                          scale=scale, clean_mask_mode=clean_mask_mode, kv_range=kv_range,
                          include_noisy_diag=include_noisy_diag, impl=impl)
@@ -455,7 +473,7 @@ def bdlm_attn_bwd_packed(q_clean, k_clean, v_clean, q_noisy, k_noisy, v_noisy, o
     entries of a stream that was left out are None.  dk_clean/dv_clean are this call's contribution for
     every clean key.  `single_pass` as in bdlm_attn_bwd."""
     if docs is not None:
-        _check_docs(docs, k_clean, kv_chunks)
+        _check_docs(docs, k_clean, kv_chunks, q_noisy, block_size, block_prefix)
     p, g = _packed_setup(q_clean, k_clean, q_noisy, block_size, block_prefix, clean_q_pos0, window, kv_chunks,
                          scale=scale, clean_mask_mode=clean_mask_mode, impl=impl, bwd_passes=passes,
                          bwd_single_pass=single_pass)

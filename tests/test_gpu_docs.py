@@ -377,3 +377,23 @@ def test_refusals():
         binding.bdlm_attn_fwd_packed(*qkv, 1, docs=binding.bdlm_doc_table([0, 255]))
     with pytest.raises(ValueError):
         binding.bdlm_attn_fwd_packed(*qkv, 1, docs=binding.bdlm_doc_table([0, 256]), kv_chunks=(128, [128, 0]))
+
+
+def test_documents_that_cut_blocks_are_refused():
+    """A noisy block over a border would attend across two documents; given by its prefix, a block belongs to the document that it
+    starts in."""
+    t, g, _ = _inputs(256, 256, 256, 2, 1, 64)
+    qkv = [g[n] for n in ("q_clean", "k_clean", "v_clean", "q_noisy", "k_noisy", "v_noisy")]
+    whole, cut, padded = (binding.bdlm_doc_table(cu, 256) for cu in ([0, 96, 96, 256], [0, 100, 256], [0, 96, 250]))
+    out = binding.bdlm_attn_fwd_packed(*qkv, 32, docs=whole)
+    for docs in (cut, padded):
+        with pytest.raises(ValueError):
+            binding.bdlm_attn_fwd_packed(*qkv, 32, docs=docs)
+        with pytest.raises(ValueError):
+            binding.bdlm_attn_bwd_packed(*qkv, *out, g["do_clean"], g["do_noisy"], 32, docs=docs)
+        prefix = torch.arange(0, 256, 32, dtype=torch.int32, device="cuda")
+        binding.bdlm_attn_fwd_packed(*qkv, 32, docs=docs, block_prefix=prefix)
+        binding.bdlm_attn_fwd_packed(*qkv[:3], None, None, None, 32, docs=docs)
+    short = [x[:, :96].contiguous() for x in qkv[3:]]
+    binding.bdlm_attn_fwd_packed(*qkv[:3], *short, 32, docs=padded)   # no block over its end
+    torch.cuda.synchronize()

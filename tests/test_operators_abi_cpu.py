@@ -129,3 +129,15 @@ def test_document_starts_are_checked_on_the_host():
             binding.bdlm_doc_table(bad)
     with pytest.raises(ValueError):
         binding.bdlm_doc_table([0, 100], 50)
+
+
+def test_documents_that_cut_blocks_are_found():
+    """Without block_prefix the blocks lie over the positions, and one that a document's border cuts would mix two documents."""
+    buffer = torch.zeros(2 * 101, dtype=torch.int32)
+    table = lambda *borders: binding.DocTable(buffer, 100, 100, 0, torch.tensor(borders))
+    assert table(0, 32, 96).first_cut(32, 96) is None and table(0, 32, 96).first_cut(16, 96) is None
+    assert table(0, 32, 50, 96).first_cut(32, 96) == 50
+    assert table(10, 96).first_cut(32, 96) == 10       # positions of no document before the first
+    assert table(0, 90).first_cut(32, 96) == 90        # and behind the last
+    assert table(0, 90).first_cut(32, 64) is None      # no block lies there
+    assert binding.DocTable(buffer, 100, 100, 0).first_cut(32, 96) is None   # borders not known
