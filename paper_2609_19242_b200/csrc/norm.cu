@@ -685,13 +685,15 @@ void by_types(const bdlm_norm_params* p, const Layout& l, F f) {
   else if (p->dtype == BDLM_FP16) by_weight(Type<__half>{});
   else by_shift(Type<float>{}, Type<float>{});
 }
+// smem: bytes a thread.  The limit that is set is the one of the largest CTA, the same in every call: the attribute is the function's,
+// and another host thread may set it between this call's setting and its launch.
 template <class K>
 cudaError_t launch_rows(K kern, const Layout& l, int groups, int smem, cudaStream_t st, const NormArgs& a) {
   if (smem > 0) {
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem * BWD_THREADS);
     if (e != cudaSuccess) return e;
   }
-  return launch_chained(kern, false, (unsigned)(groups * l.team), l.rows * l.tpr, smem, st, l.team, a);
+  return launch_chained(kern, false, (unsigned)(groups * l.team), l.rows * l.tpr, smem * l.rows * l.tpr, st, l.team, a);
 }
 
 }  // namespace
@@ -781,7 +783,7 @@ int bdlm_norm_bwd(const bdlm_norm_params* p, const void* dy, const void* h, cons
                                : l.span == WIDE ? norm_bwd_kernel<X, Wt, V, I, WIDE, SH>
                                : l.items == 1   ? norm_bwd_kernel<X, Wt, V, 1, NARROW, SH>
                                                 : norm_bwd_kernel<X, Wt, V, I, NARROW, SH>;
-      e = launch_rows(kern, l, groups, (ring_of(V) * 3 + (SH ? 1 : 0)) * l.items * l.rows * l.tpr * 16, st, a);
+      e = launch_rows(kern, l, groups, (ring_of(V) * 3 + (SH ? 1 : 0)) * l.items * 16, st, a);
     });
     if (e != cudaSuccess) return BDLM_ERR_CUDA;
   }

@@ -4,6 +4,9 @@ Tolerances.  An output of type t is rounded once: eps(t)/2 of its value.  Before
 over at most 64 terms in a thread and then pairwise over at most 1024 threads (10 additions), so a sum is off by at most
 80 x 2^-24 of the sum of its terms' magnitudes; SLACK = 128 x 2^-24 covers it with the few operations around it (the
 reciprocal square root is within 2^-21)."""
+import ctypes
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -378,3 +381,39 @@ def test_gradient_of_rows_far_from_a_zero_mean(T, D, dt):
     assert (np.abs(_f64(dx) - rx) <= _half_ulp(dt) * (np.abs(rx) + off) + off).all()
     ow = (T / 148 + 150) * 2.0 ** -24 * np.abs(_f64(dy) * n).sum(axis=0) + (np.abs(_f64(dy)) * dn).sum(axis=0)
     assert (np.abs(_f64(dw) - rw) <= ow).all()
+
+
+def test_host_threads_with_calls_of_one_kernel_and_different_sizes():
+    """The backward's shared memory follows from the call's rows.  Four threads, each with a stream of its own and its arguments ready, call
+    the same kernel with little of it and with much."""
+    jobs = []
+    for T, D in ((148, 1032), (300, 4096)) * 2:
+        i = _inputs(T, D, BF16, BF16)
+        _, _, mean, rstd = binding.bdlm_norm_fwd(i["x"], i["w"], i["b"])
+        want = binding.bdlm_norm_bwd(i["dy"], i["x"], i["w"], mean, rstd, bias=True)
+        out = tuple(torch.empty_like(t) for t in want)
+        p = binding.make_norm_params(T, D, BF16, BF16)
+        ws = torch.empty(binding.bdlm_norm_workspace_bytes(p), dtype=torch.uint8, device="cuda")
+        stream = torch.cuda.Stream()
+        args = [ctypes.byref(p)] + [ctypes.c_void_p(t.data_ptr()) for t in (i["dy"], i["x"], i["w"], mean, rstd)] + [None]
+        args += [ctypes.c_void_p(t.data_ptr()) for t in (*out, ws)] + [ctypes.c_size_t(ws.numel()), ctypes.c_void_p(stream.cuda_stream)]
+        jobs.append((args, out, want, (i, mean, rstd, p, ws, stream)))
+    torch.cuda.synchronize()
+    bwd, failed, start = binding.lib().bdlm_norm_bwd, [], threading.Barrier(len(jobs))
+
+    def work(args):
+        start.wait()
+        for _ in range(20000):
+            rc = bwd(*args)
+            if rc != 0:
+                failed.append(rc)
+                return
+    threads = [threading.Thread(target=work, args=(j[0],)) for j in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not failed, failed
+    for _, out, want, _ in jobs:
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
