@@ -32,7 +32,7 @@ extern "C" {
 #endif
 
 typedef struct {
-  int32_t T, D, V;       /* T >= 0; D, V >= 1; T and V at most 2^30 */
+  int32_t T, D, V;       /* T >= 0; D, V >= 1; each at most 2^30 */
   int32_t table_dtype;   /* BDLM_BF16, BDLM_FP16 or BDLM_FP32 */
   int32_t out_dtype;
   float   scale;         /* finite */

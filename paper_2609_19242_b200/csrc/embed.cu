@@ -525,8 +525,9 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) embed_join_kernel(const SumAr
 }
 
 // ------------------------------------------------------------------------------------------------ host
+// (D: columns are counted in 32 bits, and steps of a few thousand go past the last one)
 int check(const bdlm_embed_params* p) {
-  if (p == nullptr || p->T < 0 || p->D <= 0 || p->V <= 0 || p->T > (1 << 30) || p->V > (1 << 30)) return BDLM_ERR_INVALID_ARG;
+  if (p == nullptr || p->T < 0 || p->D <= 0 || p->V <= 0 || p->T > (1 << 30) || p->V > (1 << 30) || p->D > (1 << 30)) return BDLM_ERR_INVALID_ARG;
   if (p->table_dtype < BDLM_BF16 || p->table_dtype > BDLM_FP32 || p->out_dtype < BDLM_BF16 || p->out_dtype > BDLM_FP32) return BDLM_ERR_INVALID_ARG;
   if (p->out_dtype != p->table_dtype && p->table_dtype != BDLM_FP32) return BDLM_ERR_INVALID_ARG;
   if (!isfinite(p->scale) || (p->accumulate != 0 && p->accumulate != 1) || p->reserved != 0) return BDLM_ERR_INVALID_ARG;

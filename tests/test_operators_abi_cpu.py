@@ -141,3 +141,12 @@ def test_documents_that_cut_blocks_are_found():
     assert table(0, 90).first_cut(32, 96) == 90        # and behind the last
     assert table(0, 90).first_cut(32, 64) is None      # no block lies there
     assert binding.DocTable(buffer, 100, 100, 0).first_cut(32, 96) is None   # borders not known
+
+
+@pytest.mark.parametrize("D", [(1 << 30) + 1, 2 ** 31 - 1])
+def test_embed_rows_too_long_to_count(D):
+    L, p = binding.lib(), _embed(D=D, V=1)
+    assert L.bdlm_embed_fwd(ctypes.byref(p), OK, OK, OK, None) == -1
+    assert L.bdlm_embed_bwd(ctypes.byref(p), OK, OK, OK, OK, 1 << 60, None) == -1
+    assert binding.bdlm_embed_workspace_bytes(p) == 0
+    assert binding.bdlm_embed_workspace_bytes(_embed(D=1 << 30, V=1)) > 0
