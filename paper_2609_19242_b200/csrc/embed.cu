@@ -337,7 +337,7 @@ __global__ void __launch_bounds__(SUM_THREADS, 2) embed_sum_kernel(const SumArgs
       }
       __syncthreads();
       auto absent = [&](int r) { return !((present[r >> 5] >> (r & 31)) & 1u); };
-      if (a.D * (int)sizeof(E) <= SHORT_ROW) zero_short_rows(dtable + v0 * a.D, n, a.D, absent);
+      if (a.D <= SHORT_ROW / (int)sizeof(E)) zero_short_rows(dtable + v0 * a.D, n, a.D, absent);
       else
         for (int r = threadIdx.x >> 5; r < n; r += SUM_THREADS / 32)
           if (absent(r)) zero_row(dtable + (v0 + r) * a.D, a.D);

@@ -331,3 +331,14 @@ def test_runs_of_every_number_of_pieces(D, start):
     assert len(ids) < 8192
     _check_bwd(len(ids), D, 3 * len(lengths), FP32, FP32, ids=ids, start=start)
     _check_bwd(len(ids), D, 3 * len(lengths), BF16, BF16, ids=ids, scale=0.25, start=start)
+
+
+def test_rows_of_more_bytes_than_32_bits_count():
+    """Rows of 2^31 bytes: those of tokens that do not occur are zeroed, by whole rows and not as short ones."""
+    V, D = 4, 1 << 29
+    dout = torch.zeros(1, D, device="cuda")
+    dout[0, ::4099] = 3.0
+    grad = torch.full((V, D), 7.0, device="cuda")
+    binding.bdlm_embed_bwd(dout, torch.tensor([2], dtype=torch.int32, device="cuda"), V, out=grad)
+    for v in range(V):
+        assert torch.equal(grad[v], dout[0]) if v == 2 else not bool(grad[v].any())
