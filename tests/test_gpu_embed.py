@@ -342,3 +342,74 @@ def test_rows_of_more_bytes_than_32_bits_count():
     binding.bdlm_embed_bwd(dout, torch.tensor([2], dtype=torch.int32, device="cuda"), V, out=grad)
     for v in range(V):
         assert torch.equal(grad[v], dout[0]) if v == 2 else not bool(grad[v].any())
+
+
+# More than 8192 tokens are sorted by digits of nine bits or fewer, by one cluster; the calls above reach it with small tables alone.
+@pytest.mark.parametrize("V", [1, 511, 512, 513, 262143, 262144, 1 << 20])
+def test_sort_of_one_to_three_digits(V):
+    _check_bwd(9000, 3, V, masked=0.2)
+
+
+def test_sort_of_more_tokens_than_registers_hold():
+    """More than 65536 tokens: a thread's pairs are read again in each of the three passes."""
+    _check_bwd(70001, 3, 300000, masked=0.3)
+
+
+def test_sort_of_four_digits():
+    V, T = (1 << 27) + 5, 9000
+    rng = np.random.default_rng(0)
+    ids = np.concatenate([rng.integers(0, V, size=T - 1003), np.full(1000, V - 1), [0, V, -1]])
+    rng.shuffle(ids)
+    dout = torch.randn(T, 1, generator=torch.Generator().manual_seed(1)).cuda()
+    got = binding.bdlm_embed_bwd(dout, torch.tensor(ids, dtype=torch.int32, device="cuda"), V)
+    real = ids[(ids >= 0) & (ids < V)]
+    uniq, place = np.unique(real, return_inverse=True)
+    d64 = _f64(dout)[(ids >= 0) & (ids < V), 0]
+    ref, size = np.zeros(len(uniq)), np.zeros(len(uniq))
+    np.add.at(ref, place, d64)
+    np.add.at(size, place, np.abs(d64))
+    at = torch.from_numpy(uniq).cuda()
+    # pieces of nine tokens; a run of 1000 in sixteen shares of its 112 pieces
+    assert (np.abs(_f64(got[at, 0]) - ref) <= (9 + 112 / 16 + 16 + 1) * 2.0 ** -24 * size).all()
+    got[at] = 0.0
+    assert (got == 0).all()
+
+
+@pytest.mark.parametrize("case", ["one", "alternating", "none", "beyond", "descending", "runs", "last_only", "mixed_pads"])
+@pytest.mark.parametrize("start", [None, True])
+def test_sort_patterns_of_ids(case, start):
+    T, V = 9001, 1000
+    t = np.arange(T)
+    ids = {"one": np.full(T, 641), "alternating": t % 2 * 999, "none": np.full(T, -1), "beyond": np.where(t % 3 == 0, V, np.where(t % 3 == 1, 2 ** 31 - 1, -2 ** 31)),
+           "descending": (T - 1 - t) % V, "runs": t // 40 % V, "last_only": np.where(t == T - 1, 5, -1), "mixed_pads": np.where(t % 2 == 0, -7, t % V)}[case]
+    _check_bwd(T, 24, V, FP32, FP32, ids=ids, start=start)
+
+
+@pytest.mark.parametrize("T", [9000, 70001])
+def test_sort_under_capture_and_on_two_streams(T):
+    D, V = 40, 5000
+    dout = torch.randn(T, D, device="cuda").to(BF16)
+    a = torch.tensor(_ids(T, V, 1, 0.4), dtype=torch.int32, device="cuda")
+    b = torch.tensor(_ids(T, V, 2, 0.1), dtype=torch.int32, device="cuda")
+    want = [binding.bdlm_embed_bwd(dout, i, V) for i in (a, b)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(5):
+        for s, i in zip(streams, (a, b)):
+            with torch.cuda.stream(s):
+                got.append(binding.bdlm_embed_bwd(dout, i, V))
+    torch.cuda.synchronize()
+    for k, t in enumerate(got):
+        assert torch.equal(t, want[k % 2])
+    ids = a.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        grad = binding.bdlm_embed_bwd(dout, ids, V)
+        added = binding.bdlm_embed_bwd(dout, ids, V, out=torch.zeros_like(grad), accumulate=True)
+    for i, w in zip((a, b, a), (want[0], want[1], want[0])):
+        ids.copy_(i)
+        grad.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(grad, w) and torch.equal(added, w)
