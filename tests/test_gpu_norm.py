@@ -417,3 +417,20 @@ def test_host_threads_with_calls_of_one_kernel_and_different_sizes():
     assert not failed, failed
     for _, out, want, _ in jobs:
         assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+@pytest.mark.parametrize("D", [1, 9, 40])
+def test_short_rows_of_the_largest_calls_of_one_cta(D):
+    """As many rows as one CTA takes, and one more: up to 512 rows at once, each thread's summed over up to 64 rounds, so at most 576
+    additions one after the other (beyond the limit fewer: a CTA has T / 148 rows and 148 CTAs' sums are added in 16 shares)."""
+    for T in (32768 // D, 32768 // D + 1):
+        i = _inputs(T, D, BF16, FP32)
+        _, h, mean, rstd = binding.bdlm_norm_fwd(i["x"], i["w"], i["b"], i["res"])
+        dx, dw, db = binding.bdlm_norm_bwd(i["dy"], h, i["w"], mean, rstd, dh=i["dh"], bias=True)
+        rx, rw, rb = orc.norm_backward(_f64(i["dy"]), _f64(h), _f64(i["w"]), _f64(mean), _f64(rstd), _f64(i["dh"]), False)
+        n = (_f64(h) - _f64(mean)[:, None]) * _f64(rstd)[:, None]
+        dy, chain = np.abs(_f64(i["dy"])), 576 * 2.0 ** -24
+        assert (np.abs(_f64(dw) - rw) <= (chain + 2.0 ** -23) * (dy * np.abs(n)).sum(axis=0)).all()
+        assert (np.abs(_f64(db) - rb) <= chain * dy.sum(axis=0)).all()
+        part = binding.bdlm_norm_bwd(i["dy"][:64], h[:64], i["w"], mean[:64], rstd[:64], dh=i["dh"][:64])
+        assert torch.equal(part[0], dx[:64])
