@@ -207,6 +207,16 @@ def _checked(name, t, shape, dtype, index):
     return t.data_ptr()
 
 
+def _scratch(t, index):
+    """Address and bytes of a workspace (None: none) on this device."""
+    if t is None:
+        return None, 0
+    if t.get_device() != index:
+        raise ValueError(f"workspace: expected on cuda:{index}, got {t.device}")
+    assert t.is_contiguous(), "tensors must be contiguous CUDA tensors"
+    return t.data_ptr(), t.nbytes
+
+
 def _shape_params(q, k, block_size, **kw):
     batch, L, H, d = q.shape
     return make_params(batch, L, block_size, H, k.shape[2], d, **kw)
@@ -663,8 +673,8 @@ def bdlm_norm_bwd(dy, h, weight, mean, rstd, *, dh=None, bias=False, rms=False, 
         workspace = torch.empty(need, dtype=torch.uint8, device=h.device) if need else None
     rc = lib().bdlm_norm_bwd(at, _checked("dy", dy, shape, dtype, index), _checked("h", h, shape, dtype, index), w_at,
                              _checked("mean", mean, rows, torch.float32, index), _checked("rstd", rstd, rows, torch.float32, index),
-                             _checked("dh", dh, shape, dtype, index), dx_at, dw_at, db_at, _ptr(workspace),
-                             0 if workspace is None else workspace.numel(), torch._C._cuda_getCurrentRawStream(index))
+                             _checked("dh", dh, shape, dtype, index), dx_at, dw_at, db_at, *_scratch(workspace, index),
+                             torch._C._cuda_getCurrentRawStream(index))
     if rc != 0:
         raise BdlmError(rc, "bdlm_norm_bwd")
     return out
@@ -713,7 +723,7 @@ def bdlm_embed_bwd(dout, ids, V, *, scale=1.0, dtype=None, accumulate=False, out
         need = lib().bdlm_embed_workspace_bytes(at)
         workspace = torch.empty(need, dtype=torch.uint8, device=dout.device) if need else None
     rc = lib().bdlm_embed_bwd(at, _checked("dout", dout, shape, dout.dtype, index), ids_at, _checked("out", out, (V, D), out.dtype, index),
-                              _ptr(workspace), 0 if workspace is None else workspace.numel(), torch._C._cuda_getCurrentRawStream(index))
+                              *_scratch(workspace, index), torch._C._cuda_getCurrentRawStream(index))
     if rc != 0:
         raise BdlmError(rc, "bdlm_embed_bwd")
     return out

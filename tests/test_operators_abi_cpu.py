@@ -150,3 +150,53 @@ def test_embed_rows_too_long_to_count(D):
     assert L.bdlm_embed_bwd(ctypes.byref(p), OK, OK, OK, OK, 1 << 60, None) == -1
     assert binding.bdlm_embed_workspace_bytes(p) == 0
     assert binding.bdlm_embed_workspace_bytes(_embed(D=1 << 30, V=1)) > 0
+
+
+class _On:
+    """A tensor as the binding sees it, on a device that need not be there."""
+
+    def __init__(self, device, *shape, dtype=torch.bfloat16):
+        self.index, self.shape, self.dtype, self.device, self.is_cuda = device, torch.Size(shape), dtype, f"cuda:{device}", True
+        self.itemsize = dtype.itemsize
+
+    def get_device(self):
+        return self.index
+
+    def numel(self):
+        return self.shape.numel()
+
+    @property
+    def nbytes(self):
+        return self.numel() * self.itemsize
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return 0x1000
+
+
+def test_workspaces_are_counted_in_bytes_and_stay_on_the_calls_device(monkeypatch):
+    given = []
+
+    class Library:
+        def bdlm_norm_bwd(self, *a):
+            given.append(a[10:12])
+            return 0
+
+        def bdlm_embed_bwd(self, *a):
+            given.append(a[4:6])
+            return 0
+    monkeypatch.setattr(binding, "lib", Library)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 0, raising=False)
+    x, w, rstd, ids = _On(0, 100, 64), _On(0, 64), _On(0, 100, dtype=torch.float32), _On(0, 100, dtype=torch.int32)
+    norm = lambda ws: binding.bdlm_norm_bwd(x, x, w, rstd, rstd, out=(x, w, None), workspace=ws)
+    embed = lambda ws: binding.bdlm_embed_bwd(x, ids, 9, out=_On(0, 9, 64), workspace=ws)
+    for call in (norm, embed):
+        with pytest.raises(ValueError):
+            call(_On(1, 1 << 20, dtype=torch.uint8))
+        with pytest.raises(ValueError):
+            call(_On(-1, 1 << 20, dtype=torch.uint8))
+        call(_On(0, 1000, dtype=torch.float32))
+        assert given.pop() == (0x1000, 4000) and not given
