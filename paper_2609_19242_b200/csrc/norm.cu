@@ -50,6 +50,9 @@ constexpr int NARROW_THREADS = 128, BWD_THREADS = 512;   // of a CTA, at most
 __host__ __device__ constexpr int fwd_threads(int V, int items, Span s) { return s == NARROW ? NARROW_THREADS : V == 4 && items == 2 ? 512 : 1024; }
 // (64 registers where a row takes a CTA: 16384 x 4095 forward 242 us with 99, 144 with these)
 __host__ __device__ constexpr int fwd_ctas(int V, int items, Span s) { return s == NARROW ? (items == 4 ? 4 : 8) : V == 4 && items == 2 ? 2 : 1; }
+// One CTA an SM, said outright (0: not) where a thread has one vector: the compiler otherwise keeps to 64 registers and spills (262144 x 128
+// 69 us, 58 so; with more vectors it does not, and 16384 x 4096 is 92 us without, 93 with).
+__host__ __device__ constexpr int bwd_ctas(int items) { return items == 1 ? 1 : 0; }
 // Rows in flight in the backward: the same number of bytes for 16- and 32-bit elements.
 __host__ __device__ constexpr int ring_of(int V) { return V == 8 ? 4 : 2; }
 
@@ -378,9 +381,9 @@ __global__ void __launch_bounds__(fwd_threads(V, ITEMS, S), fwd_ctas(V, ITEMS, S
 // rate would allow 82).
 // n is formed as the forward forms it, (h - mean) rstd: h rstd - mean rstd as one fused operation saves an instruction in each of the two
 // places, but the rounding of mean rstd then stands in every n of a row (3e-5 at a mean of 1000 deviations; the subtraction is exact
-// there).  It costs nothing but for rows of one vector a thread (262144 x 128 69 us, 64 fused; all others within 1 %).
+// there).  It costs nothing that shows (16384 x 4096 92 us either way).
 template <class T, class W, int V, int ITEMS, Span S, bool SHIFT>
-__global__ void __launch_bounds__(BWD_THREADS) norm_bwd_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(BWD_THREADS, bwd_ctas(ITEMS)) norm_bwd_kernel(const NormArgs a) {
   constexpr int RING = ring_of(V);
   __shared__ __align__(8) float red[S == TEAM ? 2 * RED_FLOATS : RED_FLOATS];
   extern __shared__ uint4 ring_mem[];
