@@ -229,7 +229,8 @@ int bdlm_attn_bwd_packed(const bdlm_params* p, const bdlm_packed_geometry* g,
  *     block_prefix[b] is the document's first position).  Position L belongs to no document.  A block's own rows see one another
  *     whatever lies between them, so with block_prefix NULL (blocks one after the other over the positions) the documents have to be
  *     whole numbers of blocks: one that a border cuts would mix two documents, or a document and positions of none.  The
- *     library does not see the lengths and does not check this.
+ *     library does not see the lengths and does not check this.  In clean_mask_mode 1 the blocks of the clean stream are counted
+ *     from position 0, not from the document's first: a document's first and last blocks are what its ends leave of them.
  *   - bdlm_doc_table writes the table that the kernels read, once for a packed batch; the layers' calls, forward and
  *     backward, share it.  It is the same for all batch elements.  cu_seqlens is a DEVICE array of n_docs + 1
  *     non-decreasing int32 in [0, L] (empty documents are allowed); its values are not validated, wrong ones give wrong

@@ -406,8 +406,10 @@ class DocTable:
 def bdlm_doc_table(cu_seqlens, L=None, device=None) -> DocTable:
     """Table of the documents of a packed sequence of L clean positions (default: the last entry).  `cu_seqlens`: n + 1
     non-decreasing starts and ends in [0, L], int32, or a list; document i holds positions cu_seqlens[i] ..
-    cu_seqlens[i + 1] - 1, positions outside all of them see nothing.  Its values are checked here, on a host copy, so a CUDA
-    tensor makes the call wait for the device (hand over the host's), and the call belongs outside a stream's capture."""
+    cu_seqlens[i + 1] - 1, positions outside all of them see nothing.  Rows of such positions (padding) have to hold finite values
+    all the same: a NaN or an infinity reaches rows up to 256 positions away, in its own document or another.  The values of
+    cu_seqlens are checked here, on a host copy, so a CUDA tensor makes the call wait for the device (hand over the host's), and the
+    call belongs outside a stream's capture."""
     cu = torch.as_tensor(cu_seqlens)
     if cu.dim() != 1 or cu.numel() < 2 or cu.dtype not in (torch.int32, torch.int64):
         raise ValueError("cu_seqlens must be one-dimensional int32 (or int64) with at least two entries")
@@ -451,7 +453,9 @@ def bdlm_attn_fwd_packed(q_clean, k_clean, v_clean, q_noisy, k_noisy, v_noisy, b
     q_clean [batch, Lq, H, d] or None: clean queries at positions clean_q_pos0 .. ; q_noisy
     [batch, n_blocks*block_size, H, d] or None with k_noisy/v_noisy packed alike; k_clean/v_clean
     [batch, L, H_kv, d] complete.  `docs` (a DocTable): the sequence is made of documents, none of which sees another;
-    with q_noisy None and block_size 1 that is causal attention over prompts of different lengths.
+    with q_noisy None and block_size 1 that is causal attention over prompts of different lengths.  All rows have to hold finite
+    values, those of positions outside all documents too (see bdlm_doc_table); without block_prefix the documents have to be
+    whole numbers of blocks.
     Returns (o_clean, lse_clean, o_noisy, lse_noisy)."""
     if docs is not None:
         _check_docs(docs, k_clean, kv_chunks, q_noisy, block_size, block_prefix)

@@ -382,7 +382,8 @@ __global__ void __launch_bounds__(SUM_THREADS, 2) embed_sum_kernel(const SumArgs
     const bool follow = end == after && end != before && far_after != end;
     float acc[N];
     int run = -1;
-    // tokens in flight: what 64 registers hold.  (32 tokens of 1001 elements, added: 43 us, with more of them 16; vectors, which would
+    // tokens in flight: what 64 registers hold, but for single elements, whose addresses spill 60 to 128 bytes a thread (not the adding of
+    // few tokens).  (32 tokens of 1001 elements, added: 43 us, with more of them 16; vectors, which would
     // have to spill for it, lose: 14 tokens of 6864 11 us, 16.)
     constexpr int U = FEW && V == 1 ? (ADD ? 4 : 8) : V == 1 || ADD ? 2 : 4;
     const int64_t most = follow ? min((int64_t)a.T, last + a.piece) : last;

@@ -13,7 +13,8 @@
 //              come are copied to shared memory asynchronously, a ring of them, and a thread reads what it has copied itself,
 //              without a barrier.
 // Bound by memory, the backward nearly as much by instruction issue (61 % of the slots at 8192 x 4096).  Measured, bf16 with
-// residual, of the copy rate's floor: 16384 x 4096 forward 89 us (92 %), backward 93 (88 %); 32768 x 2048 87 (94 %), 89 (92 %);
+// residual, of the copy rate's floor, calls one after the other into outputs that are there:
+// 16384 x 4096 forward 89 us (92 %), backward 92 (89 %); 32768 x 2048 87 (94 %), 90 (91 %);
 // 8192 x 8192 93 (88 %), 102 (80 %); 4096 x 16384 102 (80 %), 128 (64 %: the cluster's exchange).  Without a residual the forward
 // moves half the bytes but has as many barriers and nearly as many instructions: 16384 x 4096 64 us, 64 % (57 as a root-mean-square
 // norm, which has one sum instead of two).  Tried and slower or no faster: in the forward the next row requested ahead where there is no residual
@@ -23,7 +24,9 @@
 //
 // Rows of a length that is no whole number of 16-byte vectors begin anywhere in a vector.  They are read as the vectors that cover
 // them, shifted by `shift` elements; a thread's rows are P apart, P the number of rows after which the shift repeats, so that
-// its columns stay its own.  (16384 x 4100: 142 us forward, 206 backward; element by element 462 and 1353.)
+// its columns stay its own.  (16384 x 4100: 142 us forward, 206 backward; element by element 462 and 1353.)  Part of what is left is the
+// layout, which counts a row with the largest shift: 4095 elements have 513 vectors, one more than 256 threads take, so the backward's CTA
+// has one row of 288 threads where 4096 elements give it two of 256.
 #include <math.h>
 
 #include "../../include/bdlm_norm.h"
@@ -172,6 +175,9 @@ struct Ring {
 
 // A cluster's barrier that orders shared memory alone, which is where the sums are: a release of everything waits for the threads' stores
 // to global memory too (backward 4096 x 16384 157 us, 136 with these fences, 128 with the exchange under the next row's products as well).
+// The release covers this CTA's own sums, written before the others read them.  The other way round, a buffer is written again after
+// others have read it, because a reader's next arrival comes after its loads have returned: every loaded sum goes through the
+// shuffles that follow it, and those stand before that arrival.
 __device__ __forceinline__ void cluster_arrive() {
   asm volatile("fence.release.sync_restrict::shared::cta.cluster;\n\tbarrier.cluster.arrive.relaxed.aligned;" ::: "memory");
 }
