@@ -36,12 +36,12 @@ NAMES6 = ["q_clean", "k_clean", "v_clean", "q_noisy", "k_noisy", "v_noisy"]
 # DRAM traffic (dram__bytes_read.sum + dram__bytes_write.sum) per launch of a kernel from a one-pass ncu capture of
 # this command, keyed by (workload, kernel), each with the digest of the kernel sources it was captured on
 # (kernel_source_digest): a figure is reported only for the build it belongs to.
-_CAPTURED_ON = "2f31cc4ed154cebe"
+_CAPTURED_ON = "1279597c3f6fb059"
 NCU_TRAFFIC = {
-    ("32k", "fwd"): {"bytes": 980215296 + 521339904, "kernel_source": _CAPTURED_ON},
-    ("32k", "bwd_fused"): {"bytes": 5519783936 + 3002078976, "kernel_source": _CAPTURED_ON},
-    ("32k", "bwd_dkdv"): {"bytes": 2408756992 + 265991424, "kernel_source": _CAPTURED_ON},
-    ("32k", "bwd_dq"): {"bytes": 1539036672 + 518338560, "kernel_source": _CAPTURED_ON},
+    ("32k", "fwd"): {"bytes": 983612928 + 521548032, "kernel_source": _CAPTURED_ON},
+    ("32k", "bwd_fused"): {"bytes": 5590038272 + 3021075712, "kernel_source": _CAPTURED_ON},
+    ("32k", "bwd_dkdv"): {"bytes": 2418651136 + 265979392, "kernel_source": _CAPTURED_ON},
+    ("32k", "bwd_dq"): {"bytes": 1543802624 + 521105664, "kernel_source": _CAPTURED_ON},
 }
 TRAFFIC_NOTE = ("dram__bytes_read.sum + dram__bytes_write.sum per launch from a one-pass ncu capture of this command on "
                 "the 32k workload")
