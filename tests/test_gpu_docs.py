@@ -397,3 +397,46 @@ def test_documents_that_cut_blocks_are_refused():
     short = [x[:, :96].contiguous() for x in qkv[3:]]
     binding.bdlm_attn_fwd_packed(*qkv[:3], *short, 32, docs=padded)   # no block over its end
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("single,window", [(True, 0), (False, 0), (True, 1700)])
+def test_both_streams_of_long_documents_on_pairs_of_ctas(single, window):
+    """Documents that begin anywhere in a pair's 256 keys, against the same documents by themselves; dK and dV have the same bits each time."""
+    L, M, cu = 7680, 32, [0, 2912, 2976, 7680]
+    t, g, _ = _inputs(L, L, L, 32, 8, 128)
+    docs = binding.bdlm_doc_table(cu)
+    out, grads = _run(g, M, docs, window=window, single_pass=single)
+    for _ in range(6):
+        _, again = _run(g, M, docs, window=window, single_pass=single)
+        for i in (1, 2, 4, 5):
+            assert torch.equal(again[i], grads[i]), i
+    for a, z in zip(cu, cu[1:]):
+        part = {k: v[:, a:z].contiguous() for k, v in g.items()}
+        ref, rgrads = _run(part, M, None, window=window, single_pass=False)
+        for s in (0, 2):   # the same products, cut into tiles elsewhere
+            assert float((out[s][:, a:z].float() - ref[s].float()).abs().max()) <= pu.TOL_O
+            assert float((out[s + 1][:, :, a:z] - ref[s + 1]).abs().max()) <= pu.TOL_LSE
+        for have, want in zip(grads, rgrads):
+            assert pu.rel_l2(synth.to_f64(have[:, a:z]), synth.to_f64(want)) <= 1e-2
+
+
+def test_more_tiles_than_a_table_orders():
+    """Past 4096 tiles of 128 positions a table holds no orders: the tiles start in their own."""
+    L = 4096 * 128 + 999
+    g = torch.Generator(device="cuda").manual_seed(0)
+    q, k, v, do = (torch.randn(1, L, h, 64, generator=g, device="cuda").to(torch.bfloat16) for h in (2, 1, 1, 2))
+    cu = sorted({0, L, *range(100, L, 311)})
+    docs = binding.bdlm_doc_table(cu)
+    assert docs.buffer.numel() == 2 * (L + 1)
+    out = binding.bdlm_attn_fwd_packed(q, k, v, None, None, None, 1, docs=docs)
+    for single in (True, False):
+        grads = binding.bdlm_attn_bwd_packed(q, k, v, None, None, None, *out, do, None, 1, docs=docs, single_pass=single)
+        for i in (0, 1, len(cu) // 2, len(cu) - 3, len(cu) - 2):
+            a, z = cu[i], cu[i + 1]
+            part = [x[:, a:z].contiguous() for x in (q, k, v, do)]
+            ref = binding.bdlm_attn_fwd_packed(*part[:3], None, None, None, 1)
+            rgrads = binding.bdlm_attn_bwd_packed(*part[:3], None, None, None, *ref, part[3], None, 1, single_pass=False)
+            assert float((out[0][:, a:z].float() - ref[0].float()).abs().max()) <= pu.TOL_O
+            assert float((out[1][:, :, a:z] - ref[1]).abs().max()) <= pu.TOL_LSE
+            for have, want in zip(grads[:3], rgrads[:3]):
+                assert pu.rel_l2(synth.to_f64(have[:, a:z]), synth.to_f64(want)) <= 1e-2
